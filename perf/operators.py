@@ -358,7 +358,7 @@ def _own_append(s):
     q, k, v = _split(s)
     rotary = Rotary(s["inv_freq"], interleaved=case["interleaved"], positions=s.get("positions"),
                     q_norm=s.get("q_norm"), k_norm=s.get("k_norm"), norm_eps=NORM_EPS)
-    rows = {} if case["new_hi"] == 1 else dict(q_starts=s["starts"], q_lens=s["new"], max_q_len=s["max_new"])
+    rows = {} if case["new_hi"] == 1 else dict(q_starts=s["starts"], q_lens=s["new"])
     s["attn"].append_paged(k, v, s["k"], s["v"], s["table"], s["lens"], q=q, q_out=s["out"], rotary=rotary, **rows)
 
 
