@@ -22,6 +22,7 @@ CTX_ERR_OOM = -6
 CTX_DTYPE_BF16 = 0
 CTX_DTYPE_F32 = 1
 
+CTX_ROTARY_INTERLEAVED = 1  # ctx_rotary flag: pairs of neighbouring dimensions
 CTX_PREFILL_SPLIT_P = 1  # ctx_prefill_attn_run flag: softmax weights as two bf16 terms
 CTX_STATIC_SCRATCH_BYTES = 16 << 20  # static workspace of ctx_decode_attn_run_static, per device
 CTX_HBM_SINK_BYTES_PER_WORKGROUP = 64
@@ -37,6 +38,7 @@ EXPORTS = (
     "ctx_decode_attn_run_static",
     "ctx_decode_attn_run_paged",
     "ctx_prefill_attn_run",
+    "ctx_kv_append_run_paged",
     "ctx_opd_loss_run",
     "ctx_rollout_simulate",
     "ctx_rollout_simulate_engine",
@@ -76,6 +78,12 @@ class OpdParams(ctypes.Structure):
 
 
 _OPD_DEFAULTS = OpdParams()
+
+
+class CtxRotary(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("q_norm", ctypes.c_void_p),
+                ("k_norm", ctypes.c_void_p), ("norm_eps", ctypes.c_float), ("rotary_dim", ctypes.c_int32),
+                ("flags", ctypes.c_uint32)]
 
 
 class RolloutConfig(ctypes.Structure):
@@ -128,6 +136,9 @@ def load_library(path: str | None = None):
     lib.ctx_prefill_attn_run.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, ctypes.c_float, ctypes.c_uint32,
                                          vp, vp]
     lib.ctx_prefill_attn_run.restype = ctypes.c_int
+    lib.ctx_kv_append_run_paged.argtypes = [vp, vp, ctypes.c_int64, vp, ctypes.c_int64, vp, ctypes.c_int64, vp, vp, i32,
+                                            vp, i32, vp, vp, vp, i32, i32, ctypes.POINTER(CtxRotary), vp, vp]
+    lib.ctx_kv_append_run_paged.restype = ctypes.c_int
     lib.ctx_opd_loss_run.argtypes = [vp, ctypes.c_int64, i32, vp, vp, vp, vp, vp, i32, i32,
                                      ctypes.POINTER(OpdParams), vp, vp, vp, vp, vp, ctypes.c_int64, vp]
     lib.ctx_opd_loss_run.restype = ctypes.c_int
@@ -195,6 +206,23 @@ def _stream_ptr(stream, device=None) -> int:
         index = torch.cuda.current_device() if device is None or device.index is None else device.index
         return torch._C._cuda_getCurrentRawStream(index)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+class Rotary:
+    """What DecodeAttention.append_paged does to queries and keys (ctx_rotary): the norm of each
+    head, if weights q_norm / k_norm (bf16 [128]) are given, then the rotation of the first
+    2 * len(inv_freq) dimensions by position * inv_freq (float32; None: no rotation), over the pairs
+    (i, i + len(inv_freq)) or, interleaved, (2 i, 2 i + 1).  positions: int32 per packed row, or
+    None: each token's position in its sequence."""
+
+    def __init__(self, inv_freq=None, interleaved: bool = False, positions=None, q_norm=None, k_norm=None,
+                 norm_eps: float = 1e-6):
+        self.inv_freq, self.interleaved, self.positions = inv_freq, interleaved, positions
+        self.q_norm, self.k_norm, self.norm_eps = q_norm, k_norm, norm_eps
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
 
 
 class DecodeAttention:
@@ -277,6 +305,88 @@ class DecodeAttention:
         if rc != CTX_OK:
             raise error_for(self.lib, rc)
         return out
+
+    def _check_pages(self, k_pages, v_pages, block_tables, seqs: int):
+        import torch
+
+        d = self.desc
+        _check_tensors(self.device, (("k_pages", k_pages, torch.bfloat16), ("v_pages", v_pages, torch.bfloat16),
+                                     ("block_tables", block_tables, torch.int32)))
+        if k_pages.dim() != 4 or k_pages.shape[1:] != (d.page_tokens, d.num_kv_heads, d.head_dim) \
+                or v_pages.shape != k_pages.shape:
+            raise ValueError(f"k_pages/v_pages must be [pages, {d.page_tokens}, {d.num_kv_heads}, {d.head_dim}]")
+        if block_tables.dim() != 2 or block_tables.shape[0] != seqs:
+            raise ValueError(f"block_tables must be [{seqs}, max_pages]")
+
+    def append_paged(self, k, v, k_pages, v_pages, block_tables, seq_lens, q=None, q_out=None, q_starts=None,
+                     q_lens=None, rotary: Rotary | None = None, stream=None):
+        """Append new tokens to paged caches (ctx_kv_append_run_paged): rows k, v [rows, Hkv, D] go to the
+        slots of each sequence's last q_lens[b] of seq_lens[b] tokens (rows q_starts[b] ..; without
+        q_starts / q_lens row b is the newest token of sequence b), and q [rows, Hq, D], if given, to
+        q_out; q and k are normed and rotated as `rotary` says.  k, v and q may be slices of wider
+        rows (heads and dimensions contiguous).  Returns q_out (allocated if None, without q None)."""
+        import torch
+
+        if self.handle is None:
+            raise RuntimeError("handle is closed")
+        d = self.desc
+        if q is None and q_out is not None:
+            raise ValueError("q_out needs q")
+        if (q_starts is None) != (q_lens is None):
+            raise ValueError("q_starts and q_lens go together")
+        rows, seqs = k.shape[0], seq_lens.shape[0]
+        strides = []
+        for name, t, heads in (("q", q, d.num_q_heads), ("k", k, d.num_kv_heads), ("v", v, d.num_kv_heads)):
+            if t is None:
+                strides.append(0)
+                continue
+            if t.dtype != torch.bfloat16:
+                raise TypeError(f"{name} must be torch.bfloat16, got {t.dtype}")
+            if not t.is_cuda or t.device.index != self.device:
+                raise ValueError(f"{name} must be on cuda:{self.device}")
+            if t.shape != (rows, heads, d.head_dim):
+                raise ValueError(f"{name} must be [{rows}, {heads}, {d.head_dim}]")
+            if (heads > 1 and t.stride(1) != d.head_dim) or t.stride(2) != 1:
+                raise ValueError(f"the heads of {name} must be contiguous within its rows")
+            # the stride of a single row says nothing
+            strides.append(t.stride(0) if rows > 1 else heads * d.head_dim)
+        self._check_pages(k_pages, v_pages, block_tables, seqs)
+        _check_tensors(self.device, (("seq_lens", seq_lens, torch.int32),))
+        if q_starts is not None:
+            _check_tensors(self.device, (("q_starts", q_starts, torch.int32), ("q_lens", q_lens, torch.int32)))
+            if q_starts.shape != (seqs,) or q_lens.shape != (seqs,) or seq_lens.shape != (seqs,):
+                raise ValueError(f"q_starts, q_lens, seq_lens must all be [{seqs}]")
+        elif seq_lens.shape != (rows,):
+            raise ValueError(f"without q_starts, seq_lens must be [{rows}]")
+        if q is not None:
+            if q_out is None:
+                q_out = torch.empty((rows, d.num_q_heads, d.head_dim), dtype=torch.bfloat16, device=q.device)
+            _check_tensors(self.device, (("q_out", q_out, torch.bfloat16),))
+            if q_out.shape != (rows, d.num_q_heads, d.head_dim):
+                raise ValueError(f"q_out must be [{rows}, {d.num_q_heads}, {d.head_dim}]")
+        r = None
+        if rotary is not None:
+            for name, t, dt, n in (("inv_freq", rotary.inv_freq, torch.float32, None),
+                                   ("positions", rotary.positions, torch.int32, rows),
+                                   ("q_norm", rotary.q_norm, torch.bfloat16, d.head_dim),
+                                   ("k_norm", rotary.k_norm, torch.bfloat16, d.head_dim)):
+                if t is None:
+                    continue
+                _check_tensors(self.device, ((name, t, dt),))
+                if t.dim() != 1 or (n is not None and t.shape[0] != n):
+                    raise ValueError(f"{name} must be a vector" + ("" if n is None else f" of {n}"))
+            freqs = rotary.inv_freq
+            r = ctypes.byref(CtxRotary(_ptr(freqs), _ptr(rotary.positions), _ptr(rotary.q_norm), _ptr(rotary.k_norm),
+                                       float(rotary.norm_eps), 0 if freqs is None else 2 * freqs.shape[0],
+                                       CTX_ROTARY_INTERLEAVED if rotary.interleaved else 0))
+        sp = _stream_ptr(stream)
+        rc = self.lib.ctx_kv_append_run_paged(
+            self.handle, _ptr(q), strides[0], k.data_ptr(), strides[1], v.data_ptr(), strides[2], k_pages.data_ptr(),
+            v_pages.data_ptr(), k_pages.shape[0], block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(),
+            _ptr(q_starts), _ptr(q_lens), seqs, rows, r, _ptr(q_out), sp)
+        if rc != CTX_OK:
+            raise error_for(self.lib, rc)
+        return q_out
 
     def prefill(self, q, k_cache, v_cache, seq_offsets, seq_lens, q_starts, q_lens, max_q_len: int,
                 scale: float, out, stream=None, split_p: bool = False):

@@ -131,7 +131,7 @@ int hip_fail(hipError_t e, const char* what) {
 
 bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0; }
 
-int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+inline int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 // Checks shared by every call on a handle; they clear the last error first.
 int check_common(ctx_decode_attn* h, int32_t num_seqs, float scale) {
