@@ -2,7 +2,9 @@
  * ctx_paged_attn.h -- operators over paged key-value caches on one AMD Instinct
  * MI355X (gfx950), beside ctx_decode_attn_run_paged: the append of new keys
  * and values with the head norm and the rotation of positions applied on the
- * way.  The handle's page_tokens P must be positive.
+ * way, and the decode step with changed scores (capped by a tanh, biased by
+ * distance, masked by a window, a prefix or documents).  The handle's
+ * page_tokens P must be positive.
  *
  * Common arguments:
  *   k_pages, v_pages  bf16 [num_pages, P, Hkv, D], D = 128
@@ -85,6 +87,46 @@ int ctx_kv_append_run_paged(ctx_decode_attn* handle, const void* q, int64_t q_st
                             const int32_t* seq_lens, const int32_t* q_starts, const int32_t* q_lens,
                             int32_t num_seqs, int32_t total_q, const ctx_rotary* rotary, void* q_out,
                             void* stream);
+
+/*
+ * Scores and masks of the call below (a HOST struct, read during
+ * the call).  A query of head h at position p has with token t of its sequence
+ *
+ *   s = scale * q . k,   then, if softcap > 0, s = softcap * tanh(s / softcap),
+ *   then, if slopes are given, s -= slopes[h] * |p - t|
+ *
+ * and sees the token if t < L_b and (t < prefix_b or max(doc, p - window + 1) <= t <= p).
+ * A prefix is thus seen by every query of its sequence, its own ones included, whatever
+ * the window and the documents are.  The output is the softmax over the seen tokens
+ * times their values; a query that sees none gets zeros.
+ */
+typedef struct {
+  float softcap;              /* > 0, or 0: no cap */
+  int32_t window;             /* > 0, or 0: no window */
+  const float* slopes;        /* float [Hq], finite, or NULL: no bias */
+  const int32_t* prefix_lens; /* int32 [num_seqs] or NULL: no prefix; a value past L_b counts as L_b */
+  const int32_t* doc_starts;  /* int32, the first token of each query's document, one per
+                                 sequence, or NULL: 0.  A value above p leaves the query its
+                                 prefix alone */
+} ctx_attn_scores;
+
+/*
+ * Queue one decode step: the newest token of every sequence (p = L_b - 1, its key
+ * and value already in the pages) attends to what it sees.  Only pages with seen
+ * tokens are read.  Uses the handle's workspace, as ctx_decode_attn_run_paged does:
+ * calls that may overlap need separate handles.
+ *
+ *   q       bf16 [num_seqs, Hq, D], contiguous
+ *   scores  as above; NULL: none
+ *   out     [num_seqs, Hq, D] of desc.out_dtype, contiguous; zeros where L_b = 0
+ * Keys and values of seen tokens must be finite; what is not seen may hold anything.
+ * With split_tokens > 0, seq_lens[b] <= max_seq_len as for ctx_decode_attn_run.
+ * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, ALIGNMENT, HIP.
+ */
+int ctx_decode_attn_run_paged_scored(ctx_decode_attn* handle, const void* q, const void* k_pages,
+                                     const void* v_pages, int32_t num_pages, const int32_t* block_tables,
+                                     int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t num_seqs,
+                                     float scale, const ctx_attn_scores* scores, void* out, void* stream);
 
 #ifdef __cplusplus
 }

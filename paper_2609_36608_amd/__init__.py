@@ -8,7 +8,7 @@ and `binding.opd_loss` are the thin ctypes wrappers used by tests and the benchm
 package loads nothing; `workloads` holds the seeded input generator.
 """
 
-__all__ = ["DecodeAttention", "CtxError", "OpdParams", "Rotary", "load_library", "opd_loss"]
+__all__ = ["AttnScores", "DecodeAttention", "CtxError", "OpdParams", "Rotary", "load_library", "opd_loss"]
 
 
 def __getattr__(name):

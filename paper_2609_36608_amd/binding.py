@@ -39,6 +39,7 @@ EXPORTS = (
     "ctx_decode_attn_run_paged",
     "ctx_prefill_attn_run",
     "ctx_kv_append_run_paged",
+    "ctx_decode_attn_run_paged_scored",
     "ctx_opd_loss_run",
     "ctx_rollout_simulate",
     "ctx_rollout_simulate_engine",
@@ -84,6 +85,11 @@ class CtxRotary(ctypes.Structure):
     _fields_ = [("inv_freq", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("q_norm", ctypes.c_void_p),
                 ("k_norm", ctypes.c_void_p), ("norm_eps", ctypes.c_float), ("rotary_dim", ctypes.c_int32),
                 ("flags", ctypes.c_uint32)]
+
+
+class CtxAttnScores(ctypes.Structure):
+    _fields_ = [("softcap", ctypes.c_float), ("window", ctypes.c_int32), ("slopes", ctypes.c_void_p),
+                ("prefix_lens", ctypes.c_void_p), ("doc_starts", ctypes.c_void_p)]
 
 
 class RolloutConfig(ctypes.Structure):
@@ -139,6 +145,9 @@ def load_library(path: str | None = None):
     lib.ctx_kv_append_run_paged.argtypes = [vp, vp, ctypes.c_int64, vp, ctypes.c_int64, vp, ctypes.c_int64, vp, vp, i32,
                                             vp, i32, vp, vp, vp, i32, i32, ctypes.POINTER(CtxRotary), vp, vp]
     lib.ctx_kv_append_run_paged.restype = ctypes.c_int
+    lib.ctx_decode_attn_run_paged_scored.argtypes = [vp, vp, vp, vp, i32, vp, i32, vp, i32, ctypes.c_float,
+                                                     ctypes.POINTER(CtxAttnScores), vp, vp]
+    lib.ctx_decode_attn_run_paged_scored.restype = ctypes.c_int
     lib.ctx_opd_loss_run.argtypes = [vp, ctypes.c_int64, i32, vp, vp, vp, vp, vp, i32, i32,
                                      ctypes.POINTER(OpdParams), vp, vp, vp, vp, vp, ctypes.c_int64, vp]
     lib.ctx_opd_loss_run.restype = ctypes.c_int
@@ -221,8 +230,35 @@ class Rotary:
         self.q_norm, self.k_norm, self.norm_eps = q_norm, k_norm, norm_eps
 
 
+class AttnScores:
+    """Scores and masks of paged attention (ctx_attn_scores): s = scale q.k, capped by
+    softcap * tanh(s / softcap), less slopes[head] * |p - t|; token t is seen from position p if
+    t < prefix_lens[sequence] or max(doc_start, p - window + 1) <= t <= p.  slopes: float32 [Hq],
+    prefix_lens: int32 [B], doc_starts: int32, one per packed row (prefill) or sequence (decode);
+    0 and None leave a part out."""
+
+    def __init__(self, softcap: float = 0.0, window: int = 0, slopes=None, prefix_lens=None, doc_starts=None):
+        self.softcap, self.window = softcap, window
+        self.slopes, self.prefix_lens, self.doc_starts = slopes, prefix_lens, doc_starts
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
+
+
+def _scores_struct(scores: AttnScores, device: int, num_q_heads: int, seqs: int, rows: int) -> CtxAttnScores:
+    import torch
+
+    for name, t, dt, n in (("slopes", scores.slopes, torch.float32, num_q_heads),
+                           ("prefix_lens", scores.prefix_lens, torch.int32, seqs),
+                           ("doc_starts", scores.doc_starts, torch.int32, rows)):
+        if t is None:
+            continue
+        _check_tensors(device, ((name, t, dt),))
+        if t.shape != (n,):
+            raise ValueError(f"{name} must be [{n}]")
+    return CtxAttnScores(float(scores.softcap), int(scores.window), _ptr(scores.slopes), _ptr(scores.prefix_lens),
+                         _ptr(scores.doc_starts))
 
 
 class DecodeAttention:
@@ -269,10 +305,11 @@ class DecodeAttention:
         return out
 
     def run_paged(self, q, k_pages, v_pages, block_tables, seq_lens, scale: float, out,
-                  k_new=None, v_new=None, stream=None):
+                  k_new=None, v_new=None, stream=None, scores: AttnScores | None = None):
         """Paged caches [num_pages, P, Hkv, D]; block_tables [B, max_pages] int32;
         optional k_new / v_new [B, Hkv, D] are appended as each sequence's
-        newest token (written into its cache slot)."""
+        newest token (written into its cache slot).  scores: the step with changed scores
+        (ctx_decode_attn_run_paged_scored), whose newest tokens are in the pages already."""
         import torch
 
         if self.handle is None:
@@ -280,6 +317,8 @@ class DecodeAttention:
         d = self.desc
         if (k_new is None) != (v_new is None):
             raise ValueError("k_new and v_new go together")
+        if scores is not None and k_new is not None:
+            raise ValueError("with scores, append the new tokens first (append_paged)")
         checks = [("q", q, torch.bfloat16), ("k_pages", k_pages, torch.bfloat16),
                   ("v_pages", v_pages, torch.bfloat16), ("block_tables", block_tables, torch.int32),
                   ("seq_lens", seq_lens, torch.int32), ("out", out, self.out_dtype)]
@@ -297,6 +336,14 @@ class DecodeAttention:
         if k_new is not None and (k_new.shape != (b, d.num_kv_heads, d.head_dim) or v_new.shape != k_new.shape):
             raise ValueError(f"k_new/v_new must be [{b}, {d.num_kv_heads}, {d.head_dim}]")
         sp = _stream_ptr(stream)
+        if scores is not None:
+            rc = self.lib.ctx_decode_attn_run_paged_scored(
+                self.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), k_pages.shape[0],
+                block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(), b, float(scale),
+                ctypes.byref(_scores_struct(scores, self.device, d.num_q_heads, b, b)), out.data_ptr(), sp)
+            if rc != CTX_OK:
+                raise error_for(self.lib, rc)
+            return out
         rc = self.lib.ctx_decode_attn_run_paged(
             self.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), block_tables.data_ptr(),
             block_tables.shape[1], seq_lens.data_ptr(), b,

@@ -13,6 +13,7 @@
 #include <cstdio>
 
 #include "ctx_decode_attn.h"
+#include "ctx_paged_attn.h"
 
 // the library's per-thread last-error message (defined with the decode entry points)
 __attribute__((visibility("hidden"))) int ctx_report_error(int code, const char* msg);
@@ -57,6 +58,26 @@ __device__ __forceinline__ s16x4 pack_bf16x4(float a, float b, float c, float d)
 }
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// tanh(y) of a wave.  Up to |y| = 0.625 an odd polynomial (least relative error,
+// 4.4e-9; 8.2e-8 in fp32), which a wave whose values all lie there takes alone: the
+// scores of a softcap of 30 or more mostly do.  Beyond, 1 - 2 / (e^2|y| + 1).
+__device__ __forceinline__ float tanh_small(float y) {
+  const float z = y * y;
+  float p = fmaf(z, -0.005704982206225395f, 0.02063908241689205f);
+  p = fmaf(p, z, -0.05373971536755562f);
+  p = fmaf(p, z, 0.13331441581249237f);
+  p = fmaf(p, z, -0.3333328068256378f);
+  return fmaf(y * z, p, y);
+}
+
+constexpr float kTanhSmall = 0.625f;
+
+__device__ __forceinline__ float tanh_any(float y) {
+  const float e = fast_exp2(fabsf(y) * 2.8853900817779268f);  // +inf far out: 1
+  const float t = copysignf(fmaf(-2.0f, __builtin_amdgcn_rcpf(e + 1.0f), 1.0f), y);
+  return fabsf(y) <= kTanhSmall ? tanh_small(y) : t;
+}
 
 // LDS transpose read (gfx950): in each 16-lane group, lane l receives element
 // l % 4 of the 8-byte rows addressed by lanes l / 4, 4 + l / 4, 8 + l / 4 and
@@ -141,6 +162,24 @@ int check_common(ctx_decode_attn* h, int32_t num_seqs, float scale) {
   if (num_seqs > h->desc.max_batch)
     return fail(CTX_ERR_CAPACITY, "num_seqs %d > max_batch %d", num_seqs, h->desc.max_batch);
   if (!std::isfinite(scale)) return fail(CTX_ERR_INVALID_ARG, "scale is not finite");
+  return CTX_OK;
+}
+
+constexpr int32_t kMostTokens = 1 << 30;  // of a sequence in paged caches: positions stay in 32 bits
+
+// Checks of what the calls over paged caches with changed scores share.
+[[maybe_unused]] int check_scored(const ctx_decode_attn* h, const ctx_attn_scores& sc, float scale,
+                                  int32_t num_pages, int32_t max_pages) {
+  if (h->desc.page_tokens <= 0) return fail(CTX_ERR_UNSUPPORTED, "the handle was created without page_tokens");
+  if (num_pages < 0 || max_pages <= 0)
+    return fail(CTX_ERR_INVALID_ARG, "num_pages must not be negative and max_pages_per_seq must be positive");
+  if ((int64_t)num_pages * h->desc.page_tokens > INT32_MAX)
+    return fail(CTX_ERR_UNSUPPORTED, "caches of more than 2^31 - 1 tokens");
+  if (!(std::isfinite(sc.softcap) && sc.softcap >= 0.f))
+    return fail(CTX_ERR_INVALID_ARG, "softcap must be finite and >= 0");
+  if (sc.softcap > 0.f && !std::isfinite(scale / sc.softcap))
+    return fail(CTX_ERR_INVALID_ARG, "scale / softcap is not finite");
+  if (sc.window < 0) return fail(CTX_ERR_INVALID_ARG, "window %d < 0", sc.window);
   return CTX_OK;
 }
 

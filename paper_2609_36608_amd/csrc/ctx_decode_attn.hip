@@ -39,6 +39,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 #include <cstdio>
@@ -46,6 +47,7 @@
 #include <new>
 
 #include "ctx_attn_common.h"
+#include "ctx_paged_attn.h"
 
 namespace {
 
@@ -85,7 +87,6 @@ struct Plan {
   int32_t forced_width;  // > 0: fixed tokens per range
   int32_t wide_from;     // most tokens of a batch in ranges of kMinRange, and of twice that
   int32_t widest_from;
-  int32_t pad;           // sequences occupy round_up(L, pad) tokens of the flattened batch
   float scale_log2;      // scale * log2(e)
 };
 
@@ -142,21 +143,70 @@ __device__ __forceinline__ float wave_max(float x) {
 // on the critical path of every wave's length scan.
 __device__ __forceinline__ int64_t padded(int64_t len, int pad) { return (len + pad - 1) & ~(int64_t)(pad - 1); }
 
-// sum of the padded lens[0 .. n)
-__device__ __forceinline__ int64_t sum_lens(const int32_t* __restrict__ lens, int n, int lane, int pad) {
+// Tokens that each sequence occupies in the flattened batch: its length, padded.
+struct PaddedLens {
+  static constexpr bool kMayBeEmpty = false;
+  const int32_t* lens;
+  int pad;
+  __device__ __forceinline__ int64_t operator()(int b) const { return padded(lens[b], pad); }
+};
+
+// What the newest token of a sequence sees of its L tokens: t < prefix and low <= t < L.
+// Whole blocks between the two are left out of the flattened batch: of its token v on,
+// v >= hole, token v + skip is meant.
+struct Seen {
+  int len;     // L
+  int prefix;  // <= L
+  int low;     // >= L: the prefix alone
+  int hole, skip;  // multiples of kBlock
+  int64_t span;    // tokens in the flattened batch, a multiple of kBlock
+  __device__ __forceinline__ int token(int v) const { return v < hole ? v : v + skip; }
+};
+
+struct SeenSpans {
+  static constexpr bool kMayBeEmpty = true;  // of tokens whose pages are in the cache
+  const int32_t* lens;
+  const int32_t* prefix_lens;  // or null
+  const int32_t* doc_starts;   // or null
+  int32_t window;              // or 0
+  int32_t most;                // tokens that a row of the block table can name
+  __device__ __forceinline__ Seen seen(int b) const {
+    Seen s;
+    const int len = lens[b];
+    s.len = len < 0 ? 0 : len < most ? len : most;
+    const int prefix = prefix_lens != nullptr ? prefix_lens[b] : 0;
+    s.prefix = prefix < 0 ? 0 : prefix < s.len ? prefix : s.len;
+    s.low = window > 0 && window < s.len ? s.len - window : 0;
+    if (doc_starts != nullptr) {
+      const int doc = doc_starts[b];
+      s.low = doc > s.low ? doc : s.low;
+    }
+    const int end = (s.len + kBlock - 1) & -kBlock;
+    const int until = s.low >= s.len ? end : s.low & -kBlock;
+    s.hole = (s.prefix + kBlock - 1) & -kBlock;
+    s.skip = until > s.hole ? until - s.hole : 0;
+    s.span = end - s.skip;
+    return s;
+  }
+  __device__ __forceinline__ int64_t operator()(int b) const { return seen(b).span; }
+};
+
+// sum of the spans of sequences 0 .. n - 1
+template <typename Spans>
+__device__ __forceinline__ int64_t sum_spans(const Spans& spans, int n, int lane) {
   int64_t acc = 0;
-  for (int i = lane; i < n; i += 64) acc += padded(lens[i], pad);
+  for (int i = lane; i < n; i += 64) acc += spans(i);
   return wave_sum(acc);
 }
 
 // First sequence b whose flattened span [P_b, P_b + L_b) contains pos; *start = P_b.
 // Returns n if none.
-__device__ int find_sequence(const int32_t* __restrict__ lens, int n, int64_t pos, int lane,
-                             int64_t* start, int pad) {
+template <typename Spans>
+__device__ int find_sequence(const Spans& spans, int n, int64_t pos, int lane, int64_t* start) {
   int64_t carry = 0;
   for (int base = 0; base < n; base += 64) {
     const int i = base + lane;
-    const int64_t len = i < n ? padded(lens[i], pad) : 0;
+    const int64_t len = i < n ? spans(i) : 0;
     int64_t incl = len;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
@@ -176,7 +226,7 @@ __device__ int find_sequence(const int32_t* __restrict__ lens, int n, int64_t po
   return n;
 }
 
-// Padded lengths of the first 64 sequences, one per lane (0 past n), with their
+// Spans of the first 64 sequences, one per lane (0 past n), with their
 // inclusive prefix sums: one load round answers totals and offsets for
 // batches of up to 64 sequences.
 struct LaneScan {
@@ -184,10 +234,10 @@ struct LaneScan {
   int64_t incl;
 };
 
-__device__ __forceinline__ LaneScan scan_lane_lens(const int32_t* __restrict__ lens, int n, int lane,
-                                                   int pad) {
+template <typename Spans>
+__device__ __forceinline__ LaneScan scan_lane_spans(const Spans& spans, int n, int lane) {
   LaneScan r;
-  r.len = lane < n ? padded(lens[lane], pad) : 0;
+  r.len = lane < n ? spans(lane) : 0;
   r.incl = wave_scan(r.len);
   return r;
 }
@@ -200,37 +250,60 @@ __device__ __forceinline__ int64_t range_width(int64_t total, const Plan& p) {
   return w < least ? least : w;
 }
 
+// Range w's tokens [ws, we) of the flattened batch and the first sequence b it
+// overlaps (its span starts at pos); false if the range is empty.
+template <typename Spans>
+__device__ __forceinline__ bool wave_range(const Spans& spans, const Plan& p, int w, int lane, int64_t* width,
+                                           int64_t* ws, int64_t* we, int* b, int64_t* pos) {
+  int64_t total;
+  if (p.num_seqs <= 64) {
+    const LaneScan sc = scan_lane_spans(spans, p.num_seqs, lane);
+    total = lane_value(sc.incl, 63);
+    *width = range_width(total, p);
+    *ws = (int64_t)w * *width;
+    if (*ws >= total) return false;
+    const unsigned long long hit = __ballot(sc.incl - sc.len <= *ws && *ws < sc.incl);
+    *b = __ffsll(hit) - 1;
+    *pos = lane_value(sc.incl - sc.len, *b);
+  } else {
+    total = sum_spans(spans, p.num_seqs, lane);
+    *width = range_width(total, p);
+    *ws = (int64_t)w * *width;
+    if (*ws >= total) return false;
+    *b = find_sequence(spans, p.num_seqs, *ws, lane, pos);
+  }
+  *we = *ws + *width < total ? *ws + *width : total;
+  return true;
+}
+
 // ------------------------------------------------------------ math helpers
 
 __device__ __forceinline__ u32x4 buf_load16(__amdgpu_buffer_rsrc_t r, int voff, int soff) {
   return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, voff, soff, kLoadAux));
 }
 
-// Process one 16-token block.  `valid` = tokens of the block inside the segment;
-// lds_v points at this lane's transpose-read address in the block's V tile
+// Process one 16-token block.  logits(x) turns the products q.k in x (lane (c, n): tokens
+// 4c + i, query n) into logits in log2 units, -inf where a token is not seen; lds_v points at this lane's transpose-read address in the block's V tile
 // (token 4c + n / 4, dimensions 4 (n % 4) .. 4 (n % 4) + 3 of dimension group 0),
 // v_step(nb) the element offset of dimension group nb from it.
+// kTerms: bf16 terms of each softmax weight, 2 (16 significant bits) or 3 (24).
+template <int kTerms, typename Logits>
 __device__ __forceinline__ void attend_block(const u32x4 (&kr)[4], const uint16_t* lds_v, const int (&v_off)[8],
-                                             const bf16x8 (&qb)[4], int valid, int c, float scale_log2,
-                                             Softmax& st, f32x4 (&o)[8]) {
+                                             const bf16x8 (&qb)[4], Logits&& logits, Softmax& st, f32x4 (&o)[8]) {
   // logits: lane (c, n) gets tokens 4c+i, query n
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int kk = 0; kk < 4; ++kk)
     s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kr[kk]), qb[kk], s, 0, 0, 0);
 
-  float x[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[i] = s[i] * scale_log2;
-    if (4 * c + i >= valid) x[i] = -INFINITY;
-  }
+  float x[4] = {s[0], s[1], s[2], s[3]};
+  logits(x);
   float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
   mx = fmaxf(mx, __shfl_xor(mx, 16));
   mx = fmaxf(mx, __shfl_xor(mx, 32));
   if (__any(mx > st.m + kLazyRescale)) {
     const float m_new = fmaxf(st.m, mx);
-    const float alpha = fast_exp2(st.m - m_new);  // 0 on the first block (m = -inf)
+    const float alpha = fast_exp2(st.m - m_new);  // 0 on the first block
 #pragma unroll
     for (int nb = 0; nb < 8; ++nb) o[nb] *= alpha;
     st.l *= alpha;
@@ -253,6 +326,15 @@ __device__ __forceinline__ void attend_block(const u32x4 (&kr)[4], const uint16_
   const s16x4 p_hi = pack_bf16x4(hi[0], hi[1], hi[2], hi[3]);
   const s16x4 p_lo = pack_bf16x4(lo[0], lo[1], lo[2], lo[3]);
   const bf16x8 pb = __builtin_bit_cast(bf16x8, __builtin_shufflevector(p_hi, p_lo, 0, 1, 2, 3, 4, 5, 6, 7));
+  // the third term, against the first of the two copies of V
+  bf16x8 pc;
+  if constexpr (kTerms == 3) {
+    float rest[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) rest[i] = lo[i] - (float)(__bf16)lo[i];
+    const s16x4 p_rest = pack_bf16x4(rest[0], rest[1], rest[2], rest[3]);
+    pc = __builtin_bit_cast(bf16x8, __builtin_shufflevector(p_rest, s16x4{0, 0, 0, 0}, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
 
   // V^T straight from the LDS tile: the transpose read gives lane (c, n)
   // V[token 4c + j][dimension 16 nb + n], j < 4, taken twice (against P_hi and P_lo)
@@ -261,9 +343,9 @@ __device__ __forceinline__ void attend_block(const u32x4 (&kr)[4], const uint16_
     const s16x4 vt = lds_read_tr16(lds_v + v_off[nb]);
     const bf16x8 va = __builtin_bit_cast(bf16x8, __builtin_shufflevector(vt, vt, 0, 1, 2, 3, 0, 1, 2, 3));
     o[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb, o[nb], 0, 0, 0);
+    if constexpr (kTerms == 3) o[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pc, o[nb], 0, 0, 0);
   }
 }
-
 
 // ------------------------------------------------------------ split kernel
 
@@ -283,6 +365,7 @@ __global__ __launch_bounds__(64 * kWgWaves) __attribute__((amdgpu_waves_per_eu(k
   // (id % kXcds) and num_ranges % kXcds == 0, so every head of a range lands on
   // the same XCD (range w on XCD w % kXcds).  Measured on MI355X this order
   // streams the cache fastest.
+  constexpr int pad = kPaged ? kBlock : 1;  // sequences start on whole blocks of paged caches
   const int wgw = (int)(blockDim.x >> 6);
   const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int hg = blockIdx.x / p.num_ranges;
@@ -295,26 +378,9 @@ __global__ __launch_bounds__(64 * kWgWaves) __attribute__((amdgpu_waves_per_eu(k
   uint16_t* lds_k = lds_tiles + (size_t)wv * (kTileBytes / 2);
   uint16_t* lds_v = lds_k + kBlock * kHeadDim;
 
-  // this wave's token range [ws, we) and the first sequence b it overlaps (span starts at pos)
-  int64_t total, width, ws, pos;
+  int64_t width, ws, we, pos;
   int b;
-  if (p.num_seqs <= 64) {
-    const LaneScan sc = scan_lane_lens(lens, p.num_seqs, lane, p.pad);
-    total = lane_value(sc.incl, 63);
-    width = range_width(total, p);
-    ws = (int64_t)w * width;
-    if (ws >= total) return;
-    const unsigned long long hit = __ballot(sc.incl - sc.len <= ws && ws < sc.incl);
-    b = __ffsll(hit) - 1;
-    pos = lane_value(sc.incl - sc.len, b);
-  } else {
-    total = sum_lens(lens, p.num_seqs, lane, p.pad);
-    width = range_width(total, p);
-    ws = (int64_t)w * width;
-    if (ws >= total) return;
-    b = find_sequence(lens, p.num_seqs, ws, lane, &pos, p.pad);
-  }
-  const int64_t we = ws + width < total ? ws + width : total;
+  if (!wave_range(PaddedLens{lens, pad}, p, w, lane, &width, &ws, &we, &b, &pos)) return;
 
   // LDS offsets of this lane's operand reads: K rows (token n, chunk 4kk + c)
   // and the V transpose reads (token 4c + n / 4, dimensions 16 nb + 4 (n % 4) ..)
@@ -456,7 +522,13 @@ __global__ __launch_bounds__(64 * kWgWaves) __attribute__((amdgpu_waves_per_eu(k
         u32x4 kr[4];
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) kr[kk] = *reinterpret_cast<const u32x4*>(&lds_k[k_off[kk]]);
-        attend_block(kr, lds_v, v_off, qb, valid, c, p.scale_log2, st, o);
+        attend_block<2>(kr, lds_v, v_off, qb, [&](float (&x)[4]) __attribute__((always_inline)) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            x[i] = x[i] * p.scale_log2;
+            if (4 * c + i >= valid) x[i] = -INFINITY;
+          }
+        }, st, o);
         blk_row = next_row;
       }
 
@@ -480,7 +552,217 @@ __global__ __launch_bounds__(64 * kWgWaves) __attribute__((amdgpu_waves_per_eu(k
         }
       }
     }
-    pos += padded(seq_len, p.pad);
+    pos += padded(seq_len, pad);
+    ++b;
+  }
+}
+
+// ------------------------------------------------------------ split kernel with changed scores
+
+// What a scored step changes of the logits.
+struct Scores {
+  float cap_in;   // scale / softcap (0: no cap)
+  float cap_out;  // softcap * log2(e)
+  const float* slopes;  // per query head, or null
+};
+
+// The step over paged caches with capped or biased scores and masks
+// (ctx_decode_attn_run_paged_scored): the split kernel's ranges, tiles and products,
+// over the blocks that each sequence's newest token sees.  Tokens of such a block
+// that are not seen (behind the sequence, between prefix and window, on a page
+// outside the cache) are zeros in the tiles and -inf among the logits, whatever the
+// pages hold there.  The running maximum starts at the lowest finite float: -inf
+// less -inf would make the weights of a block without a seen token NaN.
+// A bias changes with the distance to the last token seen instead of the query's own
+// position: the same for all tokens of a row, it does not change the softmax,
+// and logits near the largest stay small and precise.
+// fp32 outputs take three bf16 terms of each weight: the matrix cores are idle
+// most of the time (20 products per block and 8 KiB of K and V).
+template <typename OutT>
+__global__ __launch_bounds__(64 * kWgWaves) __attribute__((amdgpu_waves_per_eu(kPagedWavesPerEu))) void decode_scored_kernel(
+    const uint16_t* __restrict__ q, const uint16_t* __restrict__ kc, const uint16_t* __restrict__ vc, SeenSpans spans,
+    Plan p, Scores sco, const int32_t* __restrict__ block_tables, int32_t max_pages, int32_t num_pages,
+    int32_t page_tokens, float* __restrict__ o_ws, float2* __restrict__ ml_ws, OutT* __restrict__ out) {
+  constexpr int kTerms = sizeof(OutT) == 4 ? 3 : 2;
+  const int lane = threadIdx.x & 63;
+  const int n = lane & 15;
+  const int c = lane >> 4;
+  // workgroups, waves and tiles as in the split kernel
+  const int wgw = (int)(blockDim.x >> 6);
+  const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int hg = blockIdx.x / p.num_ranges;
+  const int w = blockIdx.x - hg * p.num_ranges;
+  const int kv = hg * wgw + wv;
+  const int g = p.group;
+  extern __shared__ __attribute__((aligned(16))) uint16_t lds_tiles[];
+  uint16_t* lds_k = lds_tiles + (size_t)wv * (kTileBytes / 2);
+  uint16_t* lds_v = lds_k + kBlock * kHeadDim;
+
+  int64_t width, ws, we, pos;
+  int b;
+  if (!wave_range(spans, p, w, lane, &width, &ws, &we, &b, &pos)) return;
+
+  int k_off[4], v_off[8];
+#pragma unroll
+  for (int kk = 0; kk < 4; ++kk) k_off[kk] = n * kHeadDim + (((4 * kk + c) ^ tile_swizzle(n)) << 3);
+  const int v_tok = 4 * c + (n >> 2);
+#pragma unroll
+  for (int nb = 0; nb < 8; ++nb)
+    v_off[nb] = v_tok * kHeadDim + (((2 * nb + ((n & 3) >> 1)) ^ tile_swizzle(v_tok)) << 3) + 4 * (n & 1);
+
+  const float slope = sco.slopes != nullptr && n < g ? sco.slopes[kv * g + n] * 1.4426950408889634f : 0.f;
+  const size_t row_elems = (size_t)p.hkv * kHeadDim;
+  const int row_bytes = (int)(row_elems * 2);
+  const int ld_tok = lane >> 4;
+  // byte offsets in the vector offset, which the range check covers whatever the range
+  int voff[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) voff[u] = (4 * u + ld_tok) * row_bytes + (lane & 15) * 16;
+  const uint16_t* const khead = kc + (size_t)kv * kHeadDim;
+  const uint16_t* const vhead = vc + (size_t)kv * kHeadDim;
+  while (b < p.num_seqs && pos < we) {
+    const Seen seen = spans.seen(b);
+    const int v0 = (int)(ws > pos ? ws - pos : 0);
+    const int v1 = (int)(we - pos < seen.span ? we - pos : seen.span);
+    if (v1 > v0) {
+      bf16x8 qb[4];
+      if (n < g) {
+        const uint16_t* qrow = q + ((size_t)b * p.hq + (size_t)kv * g + n) * kHeadDim + 8 * c;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) qb[kk] = as_bf16x8(load16(qrow + 32 * kk));
+      } else {
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) qb[kk] = as_bf16x8(u32x4{0u, 0u, 0u, 0u});
+      }
+      Softmax st{-FLT_MAX, 0.f};
+      f32x4 o[8];
+#pragma unroll
+      for (int nb = 0; nb < 8; ++nb) o[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const int nearest = seen.low < seen.len ? seen.len - 1 : seen.prefix - 1;
+
+      // first cache row of 64 blocks, one per lane; -1 where the block is on no page of the cache
+      auto block_rows = [&](int v) __attribute__((always_inline)) {
+        const int t = seen.token(v + kBlock * lane);
+        const int j = t / page_tokens;
+        int row = -1;
+        if (t < seen.len && j < max_pages) {
+          const int page = block_tables[(size_t)b * max_pages + j];
+          if (page >= 0 && page < num_pages) row = page * page_tokens + (t - j * page_tokens);
+        }
+        return row;
+      };
+      int rows = block_rows(v0), held = v0;
+      u32x4 pk[4], pv[4];
+      // Issue the loads of the block at flattened token v and return whether it is on
+      // a page; past the segment's end and outside the cache the range is empty.
+      auto issue = [&](int v) __attribute__((always_inline)) {
+        int row = -1;
+        if (v < v1) {
+          if (v - held >= 64 * kBlock) {
+            held += 64 * kBlock;
+            rows = block_rows(held);
+          }
+          row = __builtin_amdgcn_readlane(rows, (v - held) / kBlock);
+        }
+        const int left = seen.len - seen.token(v);
+        const uint32_t bytes = row < 0 ? 0u : (uint32_t)((left < kBlock ? left : kBlock) * row_bytes);
+        const size_t at = row < 0 ? 0 : (size_t)row * row_elems;
+        const __amdgpu_buffer_rsrc_t rk = make_rsrc(khead + at, bytes);
+        const __amdgpu_buffer_rsrc_t rv = make_rsrc(vhead + at, bytes);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          pk[u] = buf_load16(rk, voff[u], 0);
+          pv[u] = buf_load16(rv, voff[u], 0);
+        }
+        return row >= 0;
+      };
+      bool present = issue(v0);
+      for (int v = v0; v < v1; v += kBlock) {
+        const int t0 = seen.token(v);
+        auto is_seen = [&](int t) { return present && (t < seen.prefix || (t >= seen.low && t < seen.len)); };
+        const bool whole =
+            present && (t0 + kBlock <= seen.prefix || (t0 >= seen.low && t0 + kBlock <= seen.len));
+        {
+          // lagging waves first, as in the split kernel
+          const int done = __builtin_amdgcn_readfirstlane((int)(pos + v - ws));
+          const int quarter = __builtin_amdgcn_readfirstlane((int)(width >> 2));
+          if (done < quarter) __builtin_amdgcn_s_setprio(3);
+          else if (done < 2 * quarter) __builtin_amdgcn_s_setprio(2);
+          else if (done < 3 * quarter) __builtin_amdgcn_s_setprio(1);
+          else __builtin_amdgcn_s_setprio(0);
+        }
+        if (!whole) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            if (!is_seen(t0 + 4 * u + ld_tok)) pk[u] = pv[u] = u32x4{0u, 0u, 0u, 0u};
+        }
+        __builtin_amdgcn_wave_barrier();  // keep the previous block's LDS reads before these writes
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int tok = 4 * u + ld_tok;
+          const int slot = tok * kHeadDim + (((lane & 15) ^ tile_swizzle(tok)) << 3);
+          *reinterpret_cast<u32x4*>(&lds_k[slot]) = pk[u];
+          *reinterpret_cast<u32x4*>(&lds_v[slot]) = pv[u];
+        }
+        const bool next_present = issue(v + kBlock);
+        __builtin_amdgcn_wave_barrier();
+        u32x4 kr[4];
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) kr[kk] = *reinterpret_cast<const u32x4*>(&lds_k[k_off[kk]]);
+        attend_block<kTerms>(kr, lds_v, v_off, qb, [&](float (&x)[4]) __attribute__((always_inline)) {
+          if (sco.cap_in != 0.f) {
+            float most = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              x[i] *= sco.cap_in;
+              most = fmaxf(most, fabsf(x[i]));
+            }
+            if (__any(most > kTanhSmall)) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) x[i] = tanh_any(x[i]);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) x[i] = tanh_small(x[i]);
+            }
+          }
+          const float factor = sco.cap_in != 0.f ? sco.cap_out : p.scale_log2;
+          const int t = t0 + 4 * c;
+          if (sco.slopes != nullptr) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = fmaf(x[i], factor, -slope * (float)(nearest - t - i));
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] *= factor;
+          }
+          if (!whole) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = is_seen(t + i) ? x[i] : -INFINITY;
+          }
+        }, st, o);
+        present = next_present;
+      }
+
+      float l_tot = st.l + __shfl_xor(st.l, 16);
+      l_tot += __shfl_xor(l_tot, 32);
+      if (v0 == 0 && v1 == seen.span) {
+        // all that is seen lies in this range: final output
+        if (n < g) {
+          const float inv = l_tot != 0.f ? 1.0f / l_tot : 0.f;
+          OutT* orow = out + ((size_t)b * p.hq + (size_t)kv * g + n) * kHeadDim + 4 * c;
+#pragma unroll
+          for (int nb = 0; nb < 8; ++nb) store4<OutT>(orow + 16 * nb, o[nb] * inv);
+        }
+      } else {
+        const size_t idx = ((size_t)(w + b) * p.hkv + kv) * g + n;
+        if (n < g) {
+          float* orow = o_ws + idx * kHeadDim + 4 * c;
+#pragma unroll
+          for (int nb = 0; nb < 8; ++nb) *reinterpret_cast<f32x4*>(orow + 16 * nb) = o[nb];
+          if (c == 0) ml_ws[idx] = make_float2(st.m, l_tot);
+        }
+      }
+    }
+    pos += seen.span;
     ++b;
   }
 }
@@ -497,9 +779,9 @@ __global__ __launch_bounds__(64 * kWgWaves) __attribute__((amdgpu_waves_per_eu(k
 // from there; kMergeBatch pairs of partial outputs are in flight at once.
 constexpr int kMergeBatch = 8;
 
-template <typename OutT, int kSegWaves>
+template <typename OutT, int kSegWaves, typename Spans>
 __global__ __launch_bounds__(64 * merge_waves(kSegWaves)) void decode_merge_kernel(
-    const int32_t* __restrict__ lens, Plan p, const float* __restrict__ o_ws,
+    Spans spans, Plan p, const float* __restrict__ o_ws,
     const float2* __restrict__ ml_ws, OutT* __restrict__ out) {
   constexpr int kHeads = merge_waves(kSegWaves) / kSegWaves;  // per workgroup
   const int lane = threadIdx.x & 63;
@@ -511,17 +793,17 @@ __global__ __launch_bounds__(64 * merge_waves(kSegWaves)) void decode_merge_kern
   const int h = gw - b * p.hq;
   const int kv = h / p.group;
   const int qi = h - kv * p.group;
-  const int64_t seq_len = lens[b];
+  const int64_t span = spans(b);
   int64_t total, pos;
   if (p.num_seqs <= 64) {
-    const LaneScan sc = scan_lane_lens(lens, p.num_seqs, lane, p.pad);
+    const LaneScan sc = scan_lane_spans(spans, p.num_seqs, lane);
     total = lane_value(sc.incl, 63);
     pos = lane_value(sc.incl - sc.len, b);
   } else {
     total = 0;
     pos = 0;
     for (int i = lane; i < p.num_seqs; i += 64) {
-      const int64_t len = padded(lens[i], p.pad);
+      const int64_t len = spans(i);
       total += len;
       if (i < b) pos += len;
     }
@@ -531,13 +813,13 @@ __global__ __launch_bounds__(64 * merge_waves(kSegWaves)) void decode_merge_kern
   const int half = lane >> 5;
   const int d = (lane & 31) * 4;
   OutT* orow = out + ((size_t)b * p.hq + h) * kHeadDim + d;
-  if (seq_len <= 0) {
+  if (span <= 0) {
     if (sw == 0 && half == 0) store4<OutT>(orow, f32x4{0.f, 0.f, 0.f, 0.f});
     return;
   }
   const int64_t width = range_width(total, p);
   const int64_t wf = pos / width;
-  int64_t wl = (pos + seq_len - 1) / width;
+  int64_t wl = (pos + span - 1) / width;
   if (wf == wl) return;  // written by the split kernel
   // only reachable when seq_lens breaks the max_seq_len contract: stay in the workspace
   if (wl >= p.num_ranges) wl = p.num_ranges - 1;
@@ -602,7 +884,9 @@ __global__ __launch_bounds__(64 * merge_waves(kSegWaves)) void decode_merge_kern
       acc += ww * *reinterpret_cast<const f32x4*>(&red_o[w][d]);
     }
   }
-  if (half == 0) store4<OutT>(orow, acc * (1.0f / lsum));
+  // a sum of 0: every token seen is on a page outside the cache
+  const float inv = !Spans::kMayBeEmpty || lsum != 0.f ? 1.0f / lsum : 0.f;
+  if (half == 0) store4<OutT>(orow, acc * inv);
 }
 
 // ------------------------------------------------------------ host side
@@ -767,16 +1051,16 @@ int ctx_decode_attn_create(const ctx_decode_attn_desc* desc, ctx_decode_attn** o
 
 namespace {
 
-template <typename OutT, int kSegWaves>
-void launch_merge_of(const Plan& p, const int32_t* lens, const ctx_decode_attn* h, OutT* out, hipStream_t s) {
+template <typename OutT, int kSegWaves, typename Spans>
+void launch_merge_of(const Plan& p, const Spans& spans, const ctx_decode_attn* h, OutT* out, hipStream_t s) {
   constexpr int kHeads = merge_waves(kSegWaves) / kSegWaves;
   const dim3 grid((unsigned)(((int64_t)p.num_seqs * p.hq + kHeads - 1) / kHeads));
-  hipLaunchKernelGGL((decode_merge_kernel<OutT, kSegWaves>), grid, dim3(64 * merge_waves(kSegWaves)), 0, s, lens, p,
+  hipLaunchKernelGGL((decode_merge_kernel<OutT, kSegWaves, Spans>), grid, dim3(64 * merge_waves(kSegWaves)), 0, s, spans, p,
                      h->o_ws, h->ml_ws, out);
 }
 
-template <typename OutT>
-void launch_merge(const Plan& p, const int32_t* lens, const ctx_decode_attn* h, OutT* out, hipStream_t s) {
+template <typename OutT, typename Spans>
+void launch_merge(const Plan& p, const Spans& spans, const ctx_decode_attn* h, OutT* out, hipStream_t s) {
   // Segments of an average sequence, of which a wave has 16 in flight.  Per
   // call, 4 waves per head against 1: one sequence of 30,001 tokens 29.2 and
   // 37.6 us, 8 of 4,000..12,000 49.8 and 51.8, 32 ragged ones (9 segments) 144.0
@@ -785,14 +1069,12 @@ void launch_merge(const Plan& p, const int32_t* lens, const ctx_decode_attn* h, 
   // one of 1,000 tokens.)
   const int segs = p.num_ranges / p.num_seqs + 1;
   if (segs >= 8)
-    launch_merge_of<OutT, 4>(p, lens, h, out, s);
+    launch_merge_of<OutT, 4>(p, spans, h, out, s);
   else
-    launch_merge_of<OutT, 1>(p, lens, h, out, s);
+    launch_merge_of<OutT, 1>(p, spans, h, out, s);
 }
 
-template <bool kPaged>
-int launch(ctx_decode_attn* h, const void* q, const void* k, const void* v, const int32_t* offs,
-           const int32_t* lens, int32_t num_seqs, float scale, void* out, void* stream, const Paged& pg) {
+Plan make_plan(const ctx_decode_attn* h, int32_t num_seqs, float scale, bool paged) {
   const ctx_decode_attn_desc& d = h->desc;
   Plan p;
   p.num_seqs = num_seqs;
@@ -801,14 +1083,20 @@ int launch(ctx_decode_attn* h, const void* q, const void* k, const void* v, cons
   p.group = d.num_q_heads / d.num_kv_heads;
   p.forced_width = d.split_tokens;
   p.num_ranges = d.split_tokens > 0
-                     ? (int32_t)round_up(((int64_t)num_seqs * round_up(d.max_seq_len, kPaged ? kBlock : 1) +
+                     ? (int32_t)round_up(((int64_t)num_seqs * round_up(d.max_seq_len, paged ? kBlock : 1) +
                                           d.split_tokens - 1) / d.split_tokens, kXcds)
-                     : h->ranges_auto[kPaged ? 1 : 0];
+                     : h->ranges_auto[paged ? 1 : 0];
   p.wide_from = kWideRows * kMinRange / p.group;
   p.widest_from = kWidestRows * 2 * kMinRange / p.group;
-  p.pad = kPaged ? kBlock : 1;
   p.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  return p;
+}
 
+template <bool kPaged>
+int launch(ctx_decode_attn* h, const void* q, const void* k, const void* v, const int32_t* offs,
+           const int32_t* lens, int32_t num_seqs, float scale, void* out, void* stream, const Paged& pg) {
+  const ctx_decode_attn_desc& d = h->desc;
+  const Plan p = make_plan(h, num_seqs, scale, kPaged);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const int wgw = h->split_wgw;
   const size_t split_lds = (size_t)wgw * kTileBytes;
@@ -820,19 +1108,64 @@ int launch(ctx_decode_attn* h, const void* q, const void* k, const void* v, cons
     float* op = static_cast<float*>(out);
     hipLaunchKernelGGL((decode_split_kernel<float, kPaged>), split_grid, dim3(64 * wgw), split_lds, s, qp, kp, vp,
                        offs, lens, p, pg, h->o_ws, h->ml_ws, op);
-    launch_merge<float>(p, lens, h, op, s);
+    launch_merge<float>(p, PaddedLens{lens, kPaged ? kBlock : 1}, h, op, s);
   } else {
     uint16_t* op = static_cast<uint16_t*>(out);
     hipLaunchKernelGGL((decode_split_kernel<uint16_t, kPaged>), split_grid, dim3(64 * wgw), split_lds, s, qp, kp, vp,
                        offs, lens, p, pg, h->o_ws, h->ml_ws, op);
-    launch_merge<uint16_t>(p, lens, h, op, s);
+    launch_merge<uint16_t>(p, PaddedLens{lens, kPaged ? kBlock : 1}, h, op, s);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(e, "kernel launch");
   return CTX_OK;
 }
 
+template <typename OutT>
+void launch_scored(const ctx_decode_attn* h, const Plan& p, const Scores& sco, const SeenSpans& spans, const void* q,
+                   const void* k, const void* v, const int32_t* block_tables, int32_t max_pages, int32_t num_pages,
+                   void* out, hipStream_t s) {
+  const int wgw = h->split_wgw;
+  hipLaunchKernelGGL((decode_scored_kernel<OutT>), dim3((unsigned)(p.num_ranges * p.hkv / wgw)), dim3(64 * wgw),
+                     (size_t)wgw * kTileBytes, s, static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k),
+                     static_cast<const uint16_t*>(v), spans, p, sco, block_tables, max_pages, num_pages,
+                     h->desc.page_tokens, h->o_ws, h->ml_ws, static_cast<OutT*>(out));
+  launch_merge<OutT>(p, spans, h, static_cast<OutT*>(out), s);
+}
+
 }  // namespace
+
+extern "C" int ctx_decode_attn_run_paged_scored(ctx_decode_attn* h, const void* q, const void* k_pages,
+                                                const void* v_pages, int32_t num_pages, const int32_t* block_tables,
+                                                int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t num_seqs,
+                                                float scale, const ctx_attn_scores* scores, void* out, void* stream) {
+  int rc = check_common(h, num_seqs, scale);
+  if (rc != CTX_OK) return rc;
+  ctx_attn_scores sc{};
+  if (scores != nullptr) sc = *scores;
+  rc = check_scored(h, sc, scale, num_pages, max_pages_per_seq);
+  if (rc != CTX_OK || num_seqs == 0) return rc;
+  if (q == nullptr || k_pages == nullptr || v_pages == nullptr || block_tables == nullptr || seq_lens == nullptr ||
+      out == nullptr)
+    return fail(CTX_ERR_INVALID_ARG, "NULL data pointer");
+  if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out))
+    return fail(CTX_ERR_ALIGNMENT, "q, k_pages, v_pages and out must be 16-byte aligned");
+  rc = check_device(h);
+  if (rc != CTX_OK) return rc;
+  const Plan p = make_plan(h, num_seqs, scale, true);
+  const int64_t most = (int64_t)max_pages_per_seq * h->desc.page_tokens;
+  const SeenSpans spans{seq_lens, sc.prefix_lens, sc.doc_starts, sc.window,
+                        (int32_t)(most < kMostTokens ? most : kMostTokens)};
+  const Scores sco{sc.softcap > 0.f ? scale / sc.softcap : 0.f, (float)((double)sc.softcap * 1.4426950408889634),
+                   sc.slopes};
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (h->desc.out_dtype == CTX_DTYPE_F32)
+    launch_scored<float>(h, p, sco, spans, q, k_pages, v_pages, block_tables, max_pages_per_seq, num_pages, out, s);
+  else
+    launch_scored<uint16_t>(h, p, sco, spans, q, k_pages, v_pages, block_tables, max_pages_per_seq, num_pages, out, s);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return hip_fail(e, "kernel launch");
+  return CTX_OK;
+}
 
 extern "C" {
 

@@ -119,3 +119,45 @@ def append_reference(bt: Batch, q, k, v, inv_freq, interleaved=False, positions=
             kc[slot], ks[slot] = both(k[j], k_norm)
             vc[slot] = v[j].double()
     return qo, kc, vc, qs, ks
+
+
+def seen_tokens(length, p, window=0, prefix=0, doc=0):
+    """Tokens that a query at position p sees, as a boolean vector."""
+    t = torch.arange(max(length, 0))
+    low = max(doc, p - window + 1 if window else 0)
+    return (t < prefix) | ((t >= low) & (t <= p))
+
+
+def attention_reference(bt: Batch, scale, softcap=0.0, window=0, slopes=None, prefix=None, docs=None, per_row=True):
+    """Outputs [rows, Hq, D] in 64 bits (NaN in rows of no sequence) of every packed row against bt's
+    caches; docs per packed row, or per sequence (per_row False)."""
+    out = torch.full((bt.rows, bt.hq, D), float("nan"), dtype=torch.float64)
+    g = bt.hq // bt.hkv
+    cache = {}
+    for j, at in enumerate(bt.row_of()):
+        if at is None:
+            continue
+        b, p = at
+        n = max(bt.lens[b], 0)
+        if b not in cache:
+            kb, vb = torch.zeros((n, bt.hkv, D), dtype=torch.float64), torch.zeros((n, bt.hkv, D), dtype=torch.float64)
+            there = torch.zeros(n, dtype=torch.bool)
+            for t in range(n):
+                slot = bt.slot(b, t)
+                if slot is not None:
+                    kb[t], vb[t], there[t] = bt.k[slot].double(), bt.v[slot].double(), True
+            cache[b] = kb, vb, there
+        kb, vb, there = cache[b]
+        doc = 0 if docs is None else int(docs[j if per_row else b])
+        see = seen_tokens(n, p, window, 0 if prefix is None else int(prefix[b]), doc) & there
+        out[j] = 0
+        if not see.any():
+            continue
+        t = torch.nonzero(see)[:, 0]
+        s = torch.einsum("hgd,thd->hgt", bt.q[j].double().view(bt.hkv, g, D), kb[t]) * scale
+        if softcap:
+            s = softcap * torch.tanh(s / softcap)
+        if slopes is not None:
+            s = s - slopes.double().view(bt.hkv, g, 1) * (p - t).abs().double()
+        out[j] = torch.einsum("hgt,thd->hgd", torch.softmax(s, -1), vb[t]).reshape(bt.hq, D)
+    return out
