@@ -2,9 +2,13 @@
  * ctx_paged_attn.h -- operators over paged key-value caches on one AMD Instinct
  * MI355X (gfx950), beside ctx_decode_attn_run_paged: the append of new keys
  * and values with the head norm and the rotation of positions applied on the
- * way, and the decode step with changed scores (capped by a tanh, biased by
- * distance, masked by a window, a prefix or documents).  The handle's
- * page_tokens P must be positive.
+ * way, and the causal prefill and the decode step with changed scores (capped
+ * by a tanh, biased by distance, masked by a window, a prefix or documents).
+ *
+ * A serving loop over a handle whose page_tokens P is positive: the new tokens of a
+ * turn are appended (ctx_kv_append_run_paged), attend to the cache
+ * (ctx_prefill_attn_run_paged), and every decoded token after them is appended
+ * and attends (ctx_decode_attn_run_paged_scored).
  *
  * Common arguments:
  *   k_pages, v_pages  bf16 [num_pages, P, Hkv, D], D = 128
@@ -89,7 +93,7 @@ int ctx_kv_append_run_paged(ctx_decode_attn* handle, const void* q, int64_t q_st
                             void* stream);
 
 /*
- * Scores and masks of the call below (a HOST struct, read during
+ * Scores and masks of the two attention calls below (a HOST struct, read during
  * the call).  A query of head h at position p has with token t of its sequence
  *
  *   s = scale * q . k,   then, if softcap > 0, s = softcap * tanh(s / softcap),
@@ -105,10 +109,32 @@ typedef struct {
   int32_t window;             /* > 0, or 0: no window */
   const float* slopes;        /* float [Hq], finite, or NULL: no bias */
   const int32_t* prefix_lens; /* int32 [num_seqs] or NULL: no prefix; a value past L_b counts as L_b */
-  const int32_t* doc_starts;  /* int32, the first token of each query's document, one per
-                                 sequence, or NULL: 0.  A value above p leaves the query its
-                                 prefix alone */
+  const int32_t* doc_starts;  /* int32, the first token of each query's document, one per packed
+                                 row (prefill) or sequence (decode), or NULL: 0.  A value above p
+                                 (a padding row) leaves the query its prefix alone */
 } ctx_attn_scores;
+
+/*
+ * Queue the causal prefill of each sequence's newest tokens against its pages,
+ * which already hold their keys and values.
+ *
+ *   q       bf16 [total_q, Hq, D], contiguous
+ *   max_q_len  host bound on q_lens (sizes the grid); rows past it are not touched
+ *   scores  NULL: s = scale * q . k, every token up to p
+ *   out     [total_q, Hq, D] of desc.out_dtype, contiguous
+ * Arithmetic: fp32 scores and softmax statistics, fp32 accumulation.  With bf16
+ * outputs the softmax weights enter the product with V rounded to bf16, and each
+ * row is normalised by the sum of the rounded weights; with fp32 outputs as three
+ * bf16 terms (24 significant bits).
+ * Keys and values that some query of the sequence sees must be finite, their scores
+ * too; what no query sees may hold anything.
+ * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, ALIGNMENT, HIP.
+ */
+int ctx_prefill_attn_run_paged(ctx_decode_attn* handle, const void* q, const void* k_pages, const void* v_pages,
+                               int32_t num_pages, const int32_t* block_tables, int32_t max_pages_per_seq,
+                               const int32_t* seq_lens, const int32_t* q_starts, const int32_t* q_lens,
+                               int32_t num_seqs, int32_t total_q, int32_t max_q_len, float scale,
+                               const ctx_attn_scores* scores, void* out, void* stream);
 
 /*
  * Queue one decode step: the newest token of every sequence (p = L_b - 1, its key

@@ -39,6 +39,7 @@ EXPORTS = (
     "ctx_decode_attn_run_paged",
     "ctx_prefill_attn_run",
     "ctx_kv_append_run_paged",
+    "ctx_prefill_attn_run_paged",
     "ctx_decode_attn_run_paged_scored",
     "ctx_opd_loss_run",
     "ctx_rollout_simulate",
@@ -145,6 +146,9 @@ def load_library(path: str | None = None):
     lib.ctx_kv_append_run_paged.argtypes = [vp, vp, ctypes.c_int64, vp, ctypes.c_int64, vp, ctypes.c_int64, vp, vp, i32,
                                             vp, i32, vp, vp, vp, i32, i32, ctypes.POINTER(CtxRotary), vp, vp]
     lib.ctx_kv_append_run_paged.restype = ctypes.c_int
+    lib.ctx_prefill_attn_run_paged.argtypes = [vp, vp, vp, vp, i32, vp, i32, vp, vp, vp, i32, i32, i32, ctypes.c_float,
+                                               ctypes.POINTER(CtxAttnScores), vp, vp]
+    lib.ctx_prefill_attn_run_paged.restype = ctypes.c_int
     lib.ctx_decode_attn_run_paged_scored.argtypes = [vp, vp, vp, vp, i32, vp, i32, vp, i32, ctypes.c_float,
                                                      ctypes.POINTER(CtxAttnScores), vp, vp]
     lib.ctx_decode_attn_run_paged_scored.restype = ctypes.c_int
@@ -434,6 +438,36 @@ class DecodeAttention:
         if rc != CTX_OK:
             raise error_for(self.lib, rc)
         return q_out
+
+    def prefill_paged(self, q, k_pages, v_pages, block_tables, seq_lens, q_starts, q_lens, max_q_len: int,
+                      scale: float, out, scores: AttnScores | None = None, stream=None):
+        """Causal prefill over paged caches (ctx_prefill_attn_run_paged): q / out [rows, Hq, D];
+        sequence b's q_lens[b] queries (rows q_starts[b] ..) are the last of its seq_lens[b] tokens,
+        whose keys and values are in the pages; scores changes scores and masks."""
+        import torch
+
+        if self.handle is None:
+            raise RuntimeError("handle is closed")
+        d = self.desc
+        b = seq_lens.shape[0]
+        _check_tensors(self.device, (("q", q, torch.bfloat16), ("seq_lens", seq_lens, torch.int32),
+                                     ("q_starts", q_starts, torch.int32), ("q_lens", q_lens, torch.int32),
+                                     ("out", out, self.out_dtype)))
+        if q.dim() != 3 or q.shape[1:] != (d.num_q_heads, d.head_dim) or out.shape != q.shape:
+            raise ValueError(f"q/out must be [rows, {d.num_q_heads}, {d.head_dim}]")
+        self._check_pages(k_pages, v_pages, block_tables, b)
+        if seq_lens.shape != (b,) or q_starts.shape != (b,) or q_lens.shape != (b,):
+            raise ValueError(f"seq_lens, q_starts, q_lens must all be [{b}]")
+        sc = None
+        if scores is not None:
+            sc = ctypes.byref(_scores_struct(scores, self.device, d.num_q_heads, b, q.shape[0]))
+        rc = self.lib.ctx_prefill_attn_run_paged(
+            self.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), k_pages.shape[0],
+            block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(), q_starts.data_ptr(),
+            q_lens.data_ptr(), b, q.shape[0], int(max_q_len), float(scale), sc, out.data_ptr(), _stream_ptr(stream))
+        if rc != CTX_OK:
+            raise error_for(self.lib, rc)
+        return out
 
     def prefill(self, q, k_cache, v_cache, seq_offsets, seq_lens, q_starts, q_lens, max_q_len: int,
                 scale: float, out, stream=None, split_p: bool = False):

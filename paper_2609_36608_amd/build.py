@@ -11,8 +11,8 @@ from concurrent.futures import ThreadPoolExecutor
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "ctx_decode_attn.hip")
-SRCS = [SRC, os.path.join(PKG, "csrc", "ctx_prefill_attn.hip"), os.path.join(PKG, "csrc", "ctx_kv_append.hip"),
-        os.path.join(PKG, "csrc", "ctx_opd_loss.hip"),
+SRCS = [SRC, os.path.join(PKG, "csrc", "ctx_prefill_attn.hip"), os.path.join(PKG, "csrc", "ctx_prefill_paged.hip"),
+        os.path.join(PKG, "csrc", "ctx_kv_append.hip"), os.path.join(PKG, "csrc", "ctx_opd_loss.hip"),
         os.path.join(PKG, "csrc", "ctx_ceiling_probe.hip"), os.path.join(PKG, "csrc", "ctx_rollout_sim.cpp")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libctx_decode_attn.so")

@@ -573,9 +573,9 @@ struct Scores {
 // outside the cache) are zeros in the tiles and -inf among the logits, whatever the
 // pages hold there.  The running maximum starts at the lowest finite float: -inf
 // less -inf would make the weights of a block without a seen token NaN.
-// A bias changes with the distance to the last token seen instead of the query's own
-// position: the same for all tokens of a row, it does not change the softmax,
-// and logits near the largest stay small and precise.
+// A bias changes with the distance to the seen token where it is largest instead of the
+// query's own position: the same for all tokens of a row, it does not change the
+// softmax, and logits near the largest stay small and precise.
 // fp32 outputs take three bf16 terms of each weight: the matrix cores are idle
 // most of the time (20 products per block and 8 KiB of K and V).
 template <typename OutT>
@@ -638,7 +638,10 @@ __global__ __launch_bounds__(64 * kWgWaves) __attribute__((amdgpu_waves_per_eu(k
       f32x4 o[8];
 #pragma unroll
       for (int nb = 0; nb < 8; ++nb) o[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+      // the seen token with the largest bias
       const int nearest = seen.low < seen.len ? seen.len - 1 : seen.prefix - 1;
+      const int farthest = seen.prefix > 0 ? 0 : seen.low;
+      const int top = slope >= 0.f ? nearest : farthest;
 
       // first cache row of 64 blocks, one per lane; -1 where the block is on no page of the cache
       auto block_rows = [&](int v) __attribute__((always_inline)) {
@@ -729,7 +732,7 @@ __global__ __launch_bounds__(64 * kWgWaves) __attribute__((amdgpu_waves_per_eu(k
           const int t = t0 + 4 * c;
           if (sco.slopes != nullptr) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = fmaf(x[i], factor, -slope * (float)(nearest - t - i));
+            for (int i = 0; i < 4; ++i) x[i] = fmaf(x[i], factor, -slope * (float)(top - t - i));
           } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[i] *= factor;

@@ -1,0 +1,746 @@
+// ctx_prefill_paged.hip -- causal prefill over paged caches with capped, biased and
+// masked scores for gfx950 (MI355X), behind ctx_prefill_attn_run_paged in the C ABI
+// declared in include/ctx_paged_attn.h.
+//
+// A query at position p sees token t of its sequence if t < prefix or
+// low <= t <= p, low = max(doc, p - window + 1).  As in the contiguous prefill, the
+// columns of the 16-column MFMA tiles are the consecutive (query position, head)
+// pairs of one KV group, and 32-token K/V blocks go straight from memory into LDS:
+//   * wide workgroups: 4 waves of kTiles 16-column tiles each share every block
+//     through a three-stage tile, loaded two blocks ahead;
+//   * narrow workgroups, for calls with too few columns to fill the chip: all 4 waves
+//     cover the same kTiles tiles, each with a quarter of the blocks, its own tiles and
+//     its own running maxima; they are merged through LDS in a fixed order.
+// Per 32 tokens and 16 columns a wave computes S^T = K Q^T (8 MFMA 16x16x32), the
+// scores' changes, the mask and an online softmax, and O^T += V^T P^T (8 MFMA per
+// bf16 term of P; V^T through the LDS transpose read).
+//
+//   * Blocks: the tokens that some query of the workgroup sees are a prefix and a range
+//     further on.  Whole blocks between the two are passed over: the loop counts
+//     flattened tokens v, and token v + skip is meant from v = hole on.
+//   * Pages: the cache rows of 64 half blocks (16 tokens, always within a page) are
+//     held one per lane, and looked up again when the loop has run past them.
+//   * Masks: a block that every column of the wave sees whole is not masked; one that
+//     none sees is passed over by the wave; tokens that no query of the workgroup sees
+//     are loaded as zeros, whatever the pages hold there.
+//   * Scores are kept relative to the running maximum m (log2 units): x - m in one FMA
+//     of the product, two with a bias, so that neither the cap nor the bias needs a
+//     pass of its own, and a bias of hundreds is taken off its maximum's without a
+//     rounding between.  m moves only when a column passes it by 2^8.  A column starts
+//     without a maximum and takes its first finite one.
+//   * Biases are taken from the distance to the last token that the row sees of its
+//     prefix or to its own position, whichever applies: the same for all tokens of a
+//     row, it does not change the softmax and keeps large logits precise.
+//   * bf16 outputs: weights rounded to bf16 and normalised by the sum of the rounded
+//     ones.  fp32 outputs: three bf16 terms (24 bits), in two tiles per wave, since
+//     three would not leave registers for them.
+
+#include <hip/hip_runtime.h>
+
+#include <climits>
+#include <cmath>
+#include <cstdint>
+
+#include "ctx_attn_common.h"
+#include "ctx_paged_attn.h"
+
+namespace {
+
+// the query tiles of one (sequence, KV head) re-read the same blocks, mostly from L2
+constexpr int kLoadPolicy = 0;
+
+typedef __attribute__((address_space(3))) void lds_void;
+constexpr int kWaves = 4;
+constexpr int kBlock = 32;  // tokens
+constexpr int kHalf = 16;   // tokens of half a block: on one page
+constexpr int kBlockElems = kBlock * kHeadDim;
+constexpr int kNowhere = 0x7ffffff0;  // a byte offset past every range
+constexpr int kHeld = 64;   // half blocks whose cache rows a wave holds
+
+// what a kernel changes of the scores
+enum Change { kPlain, kBias, kCap, kCapBias };
+
+// s_waitcnt vmcnt(n) with expcnt and lgkmcnt left open
+constexpr int wait_vmcnt(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }
+
+struct PagedPlan {
+  const int32_t *block_tables, *lens, *q_starts, *q_lens;
+  const int32_t *prefix_lens, *doc_starts;  // or null
+  const float* slopes;
+  int32_t window;  // or 0
+  int32_t max_pages, num_pages, page_tokens;
+  int32_t total_q, max_q_len;
+  int32_t hq, hkv, group;
+  int32_t tiles;       // workgroups per (sequence, KV head)
+  int32_t units;       // sequences x KV heads
+  int32_t last_first;  // the tiles of a unit in falling order
+  float factor;        // of the product in log2 units, without a cap
+  float cap_in, cap_in2, cap_out;  // scale / cap, twice that and cap in log2 units
+};
+
+// Workgroup barrier with no memory fence: the caller has already waited for its own
+// loads into LDS that the other waves will read, and a fence would also wait for the
+// loads of later blocks still in flight.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_barrier" ::: "memory"); }
+
+// 16 bytes per lane from voff in r straight to LDS base + 16 * lane
+__device__ __forceinline__ void load16_to_lds(__amdgpu_buffer_rsrc_t r, uint16_t* base, int voff) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)base, 16, voff, 0, 0, kLoadPolicy);
+}
+
+// NaN-propagating maximum of 8, which gfx950 has as a three-input instruction
+__device__ __forceinline__ float max8(f32x4 a, f32x4 b) {
+  const auto mx = [](float x, float y) { return __builtin_elementwise_maximum(x, y); };
+  return mx(mx(mx(mx(a[0], a[1]), a[2]), mx(mx(a[3], b[0]), b[1])), mx(b[2], b[3]));
+}
+
+// the largest of a column, whose tokens are spread over the 4 rows of 16 lanes
+__device__ __forceinline__ float column_max(float x) {
+  const uint32_t a = __float_as_uint(x);
+  const auto rows = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+  const uint32_t b = __float_as_uint(fmaxf(__uint_as_float(rows[0]), __uint_as_float(rows[1])));
+  const auto halves = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
+}
+
+template <bool kMin>
+__device__ __forceinline__ int wave_extreme(int x) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    const int y = __shfl_xor(x, off);
+    x = kMin ? (x < y ? x : y) : (x > y ? x : y);
+  }
+  return __builtin_amdgcn_readfirstlane(x);
+}
+
+template <typename OutT, int kChange, bool kSplitKv>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void prefill_paged_kernel(
+    const uint16_t* __restrict__ q, const uint16_t* __restrict__ kc, const uint16_t* __restrict__ vc, PagedPlan pp,
+    OutT* __restrict__ out) {
+  constexpr bool kHasBias = kChange == kBias || kChange == kCapBias;
+  constexpr bool kHasCap = kChange == kCap || kChange == kCapBias;
+  constexpr int kTerms = sizeof(OutT) == 4 ? 3 : 1;
+  constexpr int kTiles = sizeof(OutT) == 4 ? 2 : 3;
+  constexpr int kCols = (kSplitKv ? 1 : kWaves) * kTiles * 16;
+  constexpr int kStagers = kSplitKv ? 1 : kWaves;  // waves that stage a block together
+  constexpr int kRounds = kHalf / (4 * kStagers);  // loads per thread and half block
+  constexpr int kLoads = 2 * kRounds;              // and block, of K and of V
+  constexpr float kHeadroom = kLazyRescale;
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col_wave = kSplitKv ? 0 : wave;
+  const int stage_wave = kSplitKv ? 0 : wave;
+  const int n = lane & 15;
+  const int c = lane >> 4;
+  const int g = pp.group;
+  // every tile of a unit on one XCD, whose L2 serves the tiles' re-reads; the last tile,
+  // which sees the most tokens, first where the grid is not resident at once
+  const int slot = blockIdx.x / kXcds;
+  const int tile = pp.last_first ? pp.tiles - 1 - slot % pp.tiles : slot % pp.tiles;
+  const int unit = (slot / pp.tiles) * kXcds + (int)(blockIdx.x % kXcds);
+  if (unit >= pp.units) return;
+  const int kv = unit % pp.hkv;
+  const int b = unit / pp.hkv;
+  const int new_tokens = pp.q_lens[b];
+  const int nq = new_tokens < pp.max_q_len ? new_tokens : pp.max_q_len;
+  const int first_q = tile * kCols / g;
+  if (first_q >= nq) return;  // the whole workgroup
+  const int row0 = pp.q_starts[b];
+  const int seq_len = pp.lens[b] < 0 ? 0 : pp.lens[b];
+  const int hist = seq_len - new_tokens;  // position of query 0
+  const int64_t named = (int64_t)pp.max_pages * pp.page_tokens;
+  const int tokens = seq_len < named ? seq_len : (int)named;  // that the table can name
+  int prefix = pp.prefix_lens != nullptr ? pp.prefix_lens[b] : 0;
+  prefix = prefix < 0 ? 0 : prefix < tokens ? prefix : tokens;
+  const size_t row_elems = (size_t)pp.hkv * kHeadDim;
+  const int row_bytes = (int)(row_elems * 2);
+  const uint16_t* const khead = kc + (size_t)kv * kHeadDim;
+  const uint16_t* const vhead = vc + (size_t)kv * kHeadDim;
+
+  constexpr int kStageElems = (kSplitKv ? kWaves : 1) * kBlockElems;
+  __shared__ __attribute__((aligned(16))) uint16_t lds_k0[kStageElems];
+  __shared__ __attribute__((aligned(16))) uint16_t lds_v0[kStageElems];
+
+  // first element of the query (and output) row of the workgroup's column col, -1 if it has none
+  auto row_at = [&](int col) -> int64_t {
+    const int at = tile * kCols + col;
+    const int qi = at / g;
+    const int64_t row = (int64_t)row0 + qi;
+    return qi < nq && row >= 0 && row < pp.total_q ? (row * pp.hq + kv * g + (at - qi * g)) * kHeadDim : -1;
+  };
+  // This lane's query column in each tile: the tokens low .. last that
+  // it sees past the prefix (low = INT_MAX: none).  `last` is also where a bias is 0.
+  int low[kTiles], last[kTiles];
+  float slope[kTiles];
+  bf16x8 qb[kTiles][4];
+  // over the wave's rows: what some row sees past the prefix, what all see
+  int some_low = INT_MAX, some_last = -1, all_low = INT_MIN, all_last = INT_MAX;
+#pragma unroll
+  for (int ct = 0; ct < kTiles; ++ct) {
+    const int col = (col_wave * kTiles + ct) * 16 + n;
+    const int64_t at = row_at(col);
+    const bool valid = at >= 0;
+    const int qi = (tile * kCols + col) / g;
+    const int head = kv * g + (tile * kCols + col - qi * g);
+    const int64_t row = (int64_t)row0 + qi;
+    low[ct] = 0;
+    last[ct] = 0;
+    slope[ct] = 0.f;
+    if (valid) {
+      const int p = hist + qi;
+      const int doc = pp.doc_starts != nullptr ? pp.doc_starts[row] : 0;
+      int lo = pp.window > 0 && p >= pp.window ? p - pp.window + 1 : 0;
+      lo = doc > lo ? doc : lo;
+      if (kHasBias) slope[ct] = pp.slopes[head] * 1.4426950408889634f;
+      const int end = p < tokens ? p : tokens - 1;  // last token past the prefix
+      if (lo <= end) {
+        low[ct] = lo;
+        last[ct] = p;
+        some_low = lo < some_low ? lo : some_low;
+        some_last = end > some_last ? end : some_last;
+      } else {
+        low[ct] = INT_MAX;
+        last[ct] = p < prefix ? p : prefix - 1;
+      }
+      all_low = low[ct] > all_low ? low[ct] : all_low;
+      all_last = last[ct] < all_last ? last[ct] : all_last;
+      const uint16_t* qrow = q + at + 8 * c;
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) qb[ct][kk] = as_bf16x8(load16(qrow + 32 * kk));
+    } else {
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) qb[ct][kk] = as_bf16x8(u32x4{0u, 0u, 0u, 0u});
+    }
+  }
+  some_low = wave_extreme<true>(some_low);
+  some_last = wave_extreme<false>(some_last);
+  all_low = wave_extreme<false>(all_low);
+  all_last = wave_extreme<true>(all_last);
+  // the same over the workgroup: the tokens it reads
+  int first = some_low, until = some_last + 1;
+  if constexpr (!kSplitKv) {
+    __shared__ int lds_seen[2][kWaves];
+    if (lane == 0) {
+      lds_seen[0][wave] = some_low;
+      lds_seen[1][wave] = some_last + 1;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      first = lds_seen[0][w] < first ? lds_seen[0][w] : first;
+      until = lds_seen[1][w] > until ? lds_seen[1][w] : until;
+    }
+    first = __builtin_amdgcn_readfirstlane(first);
+    until = __builtin_amdgcn_readfirstlane(until);
+  }
+  const int end = until > prefix ? until : prefix;  // tokens from here on are not seen
+  const int hole = (prefix + kBlock - 1) & -kBlock;
+  const int skip = first < until && (first & -kBlock) > hole ? (first & -kBlock) - hole : 0;
+  const int v_end = end - skip;
+  auto token = [&](int v) { return v < hole ? v : v + skip; };
+
+  // The maxima start at the largest bias of the column: where biases grow with the
+  // distance, the first scores are rounded near it and not near 0.
+  Softmax st[kTiles];
+  float limit[kTiles];  // relative scores above it move the maximum; -inf: there is none yet
+  f32x4 o[kTiles][8];
+#pragma unroll
+  for (int ct = 0; ct < kTiles; ++ct) {
+    st[ct] = Softmax{0.f, 0.f};
+    if (kHasBias && slope[ct] < 0.f) {
+      const int back = prefix > 0 ? last[ct] : last[ct] - (low[ct] < last[ct] ? low[ct] : last[ct]);
+      const int ahead = prefix - 1 - last[ct];
+      st[ct].m = -slope[ct] * (float)(back > ahead ? back : ahead);
+    }
+    limit[ct] = -INFINITY;
+#pragma unroll
+    for (int nb = 0; nb < 8; ++nb) o[ct][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // cache rows of the half blocks from flattened token `held` on, one per lane; -1: on no page
+  int held = 0, rows = -1;
+  auto look_up = [&](int v) __attribute__((always_inline)) {
+    held = v;
+    const int t = token(v + lane * kHalf);
+    rows = -1;
+    if (v + lane * kHalf < v_end && t < end) {
+      const int j = t / pp.page_tokens;
+      if (j < pp.max_pages) {
+        const int page = pp.block_tables[(size_t)b * pp.max_pages + j];
+        if (page >= 0 && page < pp.num_pages) rows = page * pp.page_tokens + (t - j * pp.page_tokens);
+      }
+    }
+  };
+  // A block load writes lane L's 16 bytes at LDS base + 16 L: round r of wave w fills
+  // slots 0..15 of tokens (r kStagers + w) 4 + L / 16 of a half block, so each lane fetches
+  // the chunk that the swizzle puts at its slot (the swizzle repeats every 16 tokens).
+  int offset[kRounds], lane_tok[kRounds];
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    lane_tok[r] = (r * kStagers + stage_wave) * 4 + (lane >> 4);
+    offset[r] = lane_tok[r] * row_bytes + (((lane & 15) ^ tile_swizzle(lane_tok[r])) << 4);
+  }
+  // Half h of the block at flattened token v, whose first cache row is `row`, into dst;
+  // outside the cache, past `end` and between prefix and `first` zeros are written.
+  auto load_half = [&](const uint16_t* base, int row, int v, int h, uint16_t* dst) __attribute__((always_inline)) {
+    const int t = token(v) + h * kHalf;
+    const int left = row < 0 ? 0 : end - t < kHalf ? end - t : kHalf;
+    const __amdgpu_buffer_rsrc_t rs =
+        make_rsrc(base + (row < 0 ? (size_t)0 : (size_t)row * row_elems), (uint32_t)((left < 0 ? 0 : left) * row_bytes));
+    const bool edge = t < first && t + kHalf > prefix;
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+      int off = offset[r];
+      if (edge) off = t + lane_tok[r] >= prefix && t + lane_tok[r] < first ? kNowhere : off;
+      load16_to_lds(rs, dst + h * kHalf * kHeadDim + (r * kStagers + stage_wave) * 4 * kHeadDim, off);
+    }
+  };
+  auto row_of = [&](int v, int h) {
+    const int i = (v - held) / kHalf + h;
+    return v < v_end ? __builtin_amdgcn_readlane(rows, i & (kHeld - 1)) : -1;
+  };
+
+  // per-lane LDS offsets of the operand reads within a 16-token half block
+  int k_off[4];
+#pragma unroll
+  for (int kk = 0; kk < 4; ++kk) k_off[kk] = n * kHeadDim + (((4 * kk + c) ^ tile_swizzle(n)) << 3);
+  const int v_tok = 4 * c + (n >> 2);
+  const int v_row = v_tok * kHeadDim + 4 * (n & 1);
+  const int v_swz = tile_swizzle(v_tok);
+  const int v_ch = (n & 3) >> 1;
+
+  // S^T of a staged block: tokens 16 h + 4c + i (i < 4) for every column tile
+  auto scores = [&](const uint16_t* kt, f32x4 (&sc)[kTiles][2]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      u32x4 kr[4];
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk)
+        kr[kk] = *reinterpret_cast<const u32x4*>(kt + 16 * h * kHeadDim + k_off[kk]);
+#pragma unroll
+      for (int ct = 0; ct < kTiles; ++ct) sc[ct][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+        for (int ct = 0; ct < kTiles; ++ct)
+          sc[ct][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kr[kk]), qb[ct][kk], sc[ct][h], 0, 0, 0);
+    }
+  };
+
+  // The scores in log2 units less the running maxima, -inf where a token is not seen.
+  // t0: the block's first token; absent: bit h where half h is on no page.
+  auto relative = [&](int t0, int absent, f32x4 (&sc)[kTiles][2]) __attribute__((always_inline)) {
+    if constexpr (kHasCap && kTerms == 1) {
+      // tanh(y) = 1 - 2 / (e^2y + 1): 2^-23 of the cap off, far below a bf16 weight's rounding
+#pragma unroll
+      for (int ct = 0; ct < kTiles; ++ct)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            sc[ct][h][i] = __builtin_amdgcn_rcpf(fast_exp2(sc[ct][h][i] * pp.cap_in2) + 1.0f);
+    } else if constexpr (kHasCap) {
+      float most = 0.f;
+#pragma unroll
+      for (int ct = 0; ct < kTiles; ++ct)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            sc[ct][h][i] *= pp.cap_in;
+            most = fmaxf(most, fabsf(sc[ct][h][i]));
+          }
+      const bool large = __any(most > kTanhSmall);
+#pragma unroll
+      for (int ct = 0; ct < kTiles; ++ct)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sc[ct][h][i] = large ? tanh_any(sc[ct][h][i]) : tanh_small(sc[ct][h][i]);
+    }
+    // a capped score is cap_out * tanh(y), or with the form above cap_out - 2 cap_out * sc
+    constexpr bool kTwoOver = kHasCap && kTerms == 1;
+    const float factor = kTwoOver ? -2.0f * pp.cap_out : kHasCap ? pp.cap_out : pp.factor;
+    const float shift = kTwoOver ? pp.cap_out : 0.f;
+    const bool whole = absent == 0 && (t0 + kBlock <= prefix || (t0 >= all_low && t0 + kBlock - 1 <= all_last));
+    const bool before = t0 + kBlock - 1 <= all_last;  // no token lies behind a query
+    if (!kHasBias || before) {
+#pragma unroll
+      for (int ct = 0; ct < kTiles; ++ct) {
+        const float less = shift - st[ct].m;
+        const float base = kHasBias ? fmaf(slope[ct], (float)(t0 + 4 * c - last[ct]), less) : less;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            sc[ct][h][i] =
+                fmaf(sc[ct][h][i], factor, kHasBias ? fmaf(slope[ct], (float)(16 * h + i), base) : base);
+      }
+    } else {
+#pragma unroll
+      for (int ct = 0; ct < kTiles; ++ct) {
+        const int d = t0 + 4 * c - last[ct];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            sc[ct][h][i] = fmaf(sc[ct][h][i], factor, fmaf(-slope[ct], fabsf((float)(d + 16 * h + i)), shift - st[ct].m));
+      }
+    }
+    if (!whole) {
+#pragma unroll
+      for (int ct = 0; ct < kTiles; ++ct)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int t = t0 + 16 * h + 4 * c + i;
+            const bool see = (t < prefix || (t >= low[ct] && t <= last[ct])) && !(absent >> h & 1);
+            sc[ct][h][i] = see ? sc[ct][h][i] : -INFINITY;
+          }
+    }
+  };
+  // raises the maxima where a score passes its limit
+  auto raise = [&](f32x4 (&sc)[kTiles][2]) __attribute__((always_inline)) {
+    float lm[kTiles];
+    bool over = false;
+#pragma unroll
+    for (int ct = 0; ct < kTiles; ++ct) {
+      lm[ct] = max8(sc[ct][0], sc[ct][1]);
+      over = over || lm[ct] > limit[ct];
+    }
+    if (!__any(over)) return;
+#pragma unroll
+    for (int ct = 0; ct < kTiles; ++ct) {
+      if (!__any(lm[ct] > limit[ct])) continue;
+      const float top = column_max(lm[ct]);
+      const bool unset = limit[ct] < 0.f;
+      // what the rounded sum really moves by, so that a large maximum loses nothing
+      const float m = st[ct].m + (unset ? (top > -INFINITY ? top : 0.f) : fmaxf(top, 0.f));
+      const float delta = m - st[ct].m;
+      const float alpha = unset ? 1.f : fast_exp2(-delta);
+      limit[ct] = unset && !(top > -INFINITY) ? -INFINITY : kHeadroom;
+      st[ct].m = m;
+      st[ct].l *= alpha;
+#pragma unroll
+      for (int nb = 0; nb < 8; ++nb) o[ct][nb] *= alpha;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) sc[ct][h] -= delta;
+    }
+  };
+  // the softmax weights as kTerms bf16 terms
+  auto weights = [&](const f32x4 (&sc)[kTiles][2], u32x4 (&pt)[kTerms][kTiles]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int ct = 0; ct < kTiles; ++ct) {
+      float pr[8];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pr[4 * h + i] = fast_exp2(sc[ct][h][i]);
+      if constexpr (kTerms == 1) {
+        // the row sum adds the rounded weights that the product uses, a pair per dot product with (1, 1)
+        const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+        float l = st[ct].l;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bf16x2 pair = {(__bf16)pr[2 * j], (__bf16)pr[2 * j + 1]};  // round to nearest even
+          pt[0][ct][j] = __builtin_bit_cast(uint32_t, pair);
+          l = __builtin_amdgcn_fdot2_f32_bf16(pair, ones, l, false);
+        }
+        st[ct].l = l;
+      } else {
+        st[ct].l += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
+#pragma unroll
+        for (int k = 0; k < kTerms; ++k)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t w = pack_bf16x2(pr[2 * j], pr[2 * j + 1]);
+            pt[k][ct][j] = w;
+            pr[2 * j] -= __uint_as_float(w << 16);  // exact
+            pr[2 * j + 1] -= __uint_as_float(w & 0xffff0000u);
+          }
+      }
+    }
+  };
+  // O^T += V^T P^T: the K dimension holds tokens 4c .. 4c + 3 of both halves.  Raised wave
+  // priority over the product stream, and the V^T reads of one dimension group ahead of
+  // their products, as in the contiguous prefill.
+  auto values = [&](const uint16_t* vt, const u32x4 (&pt)[kTerms][kTiles]) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_setprio(1);
+    auto read_vt = [&](int nb, s16x4& v0, s16x4& v1) {
+      const int off = v_row + (((2 * nb + v_ch) ^ v_swz) << 3);
+      v0 = lds_read_tr16(vt + off);
+      v1 = lds_read_tr16(vt + 16 * kHeadDim + off);
+    };
+    s16x4 nv0, nv1;
+    read_vt(0, nv0, nv1);
+#pragma unroll
+    for (int nb = 0; nb < 8; ++nb) {
+      const bf16x8 va = __builtin_bit_cast(bf16x8, __builtin_shufflevector(nv0, nv1, 0, 1, 2, 3, 4, 5, 6, 7));
+      if (nb + 1 < 8) read_vt(nb + 1, nv0, nv1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int k = 0; k < kTerms; ++k)
+#pragma unroll
+        for (int ct = 0; ct < kTiles; ++ct)
+          o[ct][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, as_bf16x8(pt[k][ct]), o[ct][nb], 0, 0, 0);
+    }
+    __builtin_amdgcn_s_setprio(0);
+  };
+  // whether some row of the wave sees some token of the block at t0
+  auto any_seen = [&](int t0) { return t0 < prefix || (t0 <= some_last && t0 + kBlock > some_low); };
+
+  look_up(0);
+  if constexpr (!kSplitKv) {
+    __shared__ __attribute__((aligned(16))) uint16_t lds_k1[kStageElems];
+    __shared__ __attribute__((aligned(16))) uint16_t lds_v1[kStageElems];
+    __shared__ __attribute__((aligned(16))) uint16_t lds_k2[kStageElems];
+    __shared__ __attribute__((aligned(16))) uint16_t lds_v2[kStageElems];
+    int absent = 0;  // bits 2j, 2j + 1: of the block j steps on
+    auto issue = [&](int v, uint16_t* dk, uint16_t* dv, int ahead) __attribute__((always_inline)) {
+      if (v < v_end && v - held >= kHeld * kHalf) look_up(v);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int row = row_of(v, h);
+        absent |= (row < 0 ? 1 : 0) << (2 * ahead + h);
+        load_half(khead, row, v, h, dk);
+        load_half(vhead, row, v, h, dv);
+      }
+    };
+    // One block: wait for this wave's loads of it, then the barrier (every wave's loads
+    // have landed, and every wave is done with the stage read in the previous step); the
+    // loads of the block two ahead go into that stage.  The three stages are distinct LDS
+    // arrays named at compile time, so the compiler's wait before the reads covers only
+    // this stage's loads.
+    auto step = [&](int v, const uint16_t* kt, const uint16_t* vt, uint16_t* nk, uint16_t* nv) __attribute__((always_inline)) {
+      __builtin_amdgcn_s_waitcnt(wait_vmcnt(2 * kLoads));
+      lds_barrier();
+      const int gone = absent & 3;
+      absent >>= 2;
+      issue(v + 2 * kBlock, nk, nv, 1);
+      const int t0 = token(v);
+      if (v < v_end && any_seen(t0)) {
+        f32x4 sc[kTiles][2];
+        u32x4 pt[kTerms][kTiles];
+        scores(kt, sc);
+        relative(t0, gone, sc);
+        raise(sc);
+        weights(sc, pt);
+        values(vt, pt);
+      }
+    };
+    issue(0, lds_k0, lds_v0, 0);
+    issue(kBlock, lds_k1, lds_v1, 1);
+    // whole rounds of three steps (an exit in the middle would make the compiler wait at
+    // the loop's head); the last of them may be on empty blocks
+    for (int v = 0; v < v_end; v += 3 * kBlock) {
+      step(v, lds_k0, lds_v0, lds_k2, lds_v2);
+      step(v + kBlock, lds_k1, lds_v1, lds_k0, lds_v0);
+      step(v + 2 * kBlock, lds_k2, lds_v2, lds_k1, lds_v1);
+    }
+    // no load may land in LDS after the workgroup has released it
+    __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
+#pragma unroll
+    for (int ct = 0; ct < kTiles; ++ct) {
+      float l_tot = st[ct].l + __shfl_xor(st[ct].l, 16);
+      l_tot += __shfl_xor(l_tot, 32);
+      const int64_t at = row_at((wave * kTiles + ct) * 16 + n);
+      if (at >= 0) {
+        const float inv = l_tot != 0.f ? 1.0f / l_tot : 0.f;
+        OutT* orow = out + at + 4 * c;
+#pragma unroll
+        for (int nb = 0; nb < 8; ++nb) store4<OutT>(orow + 16 * nb, o[ct][nb] * inv);
+      }
+    }
+  } else {
+    // Wave w takes blocks w, w + 4, w + 8, ... through its own K and V tiles.  A tile is
+    // refilled with the wave's next block as soon as it has been read.
+    constexpr int kStride = kWaves * kBlock;
+    uint16_t* const kt = lds_k0 + wave * kBlockElems;
+    uint16_t* const vt = lds_v0 + wave * kBlockElems;
+    auto fill = [&](const uint16_t* base, int v, uint16_t* dst) __attribute__((always_inline)) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) load_half(base, row_of(v, h), v, h, dst);
+    };
+    auto gone_at = [&](int v) { return (row_of(v, 0) < 0 ? 1 : 0) | (row_of(v, 1) < 0 ? 2 : 0); };
+    fill(khead, wave * kBlock, kt);
+    fill(vhead, wave * kBlock, vt);
+    int gone = gone_at(wave * kBlock);
+    for (int v = wave * kBlock; v < v_end; v += kStride) {
+      const int t0 = token(v);
+      f32x4 sc[kTiles][2];
+      u32x4 pt[kTerms][kTiles];
+      __builtin_amdgcn_s_waitcnt(wait_vmcnt(kLoads));  // this block's K; its V is still on the way
+      asm volatile("" ::: "memory");
+      scores(kt, sc);
+      // the tile's reads have returned before its refill is issued
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      const int next = v + kStride;
+      if (next < v_end && next - held >= kHeld * kHalf) look_up(next);
+      fill(khead, next, kt);
+      const int next_gone = gone_at(next);
+      relative(t0, gone, sc);
+      raise(sc);
+      weights(sc, pt);
+      __builtin_amdgcn_s_waitcnt(wait_vmcnt(kLoads));  // this block's V
+      asm volatile("" ::: "memory");
+      values(vt, pt);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      fill(vhead, next, vt);
+      gone = next_gone;
+    }
+    __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
+    __syncthreads();
+    // Merge, half of the dimensions at a time: wave w puts its columns' maxima, sums and
+    // unnormalised outputs into its part of the tiles, 16-byte chunk ch of column j at slot
+    // ch ^ (j & 15), and every thread adds up 4 dimensions of some columns in wave order.
+    constexpr int kDims = kHeadDim / 2;
+    constexpr int kChunks = kDims / 4;
+    constexpr int kPartFloats = kCols * kDims;  // then the sums, then the maxima
+    static_assert((kPartFloats + 2 * kCols) * 4 <= 2 * kBlockElems * 2,
+                  "a wave's partial results must fit half of a tile array");
+    auto part_of = [&](int w) {
+      return reinterpret_cast<float*>((w < 2 ? lds_k0 : lds_v0) + (w & 1) * 2 * kBlockElems);
+    };
+    float* const mine = part_of(wave);
+#pragma unroll
+    for (int ct = 0; ct < kTiles; ++ct) {
+      float l_tot = st[ct].l + __shfl_xor(st[ct].l, 16);
+      l_tot += __shfl_xor(l_tot, 32);
+      if (c == 0) {
+        mine[kPartFloats + ct * 16 + n] = l_tot;
+        mine[kPartFloats + kCols + ct * 16 + n] = limit[ct] < 0.f ? -INFINITY : st[ct].m;
+      }
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      if (half > 0) __syncthreads();  // the first half has been read
+#pragma unroll
+      for (int ct = 0; ct < kTiles; ++ct)
+#pragma unroll
+        for (int nb = 0; nb < 4; ++nb)
+          *reinterpret_cast<f32x4*>(mine + (ct * 16 + n) * kDims + (((4 * nb + c) ^ n) << 2)) = o[ct][4 * half + nb];
+      __syncthreads();
+      const int ch = tid % kChunks;
+#pragma unroll
+      for (int j = tid / kChunks; j < kCols; j += 64 * kWaves / kChunks) {
+        const int64_t at = row_at(j);
+        if (at < 0) continue;
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, part_of(w)[kPartFloats + kCols + j]);
+        float l = 0.f;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          const float m = part_of(w)[kPartFloats + kCols + j];
+          const float share = m > -INFINITY ? fast_exp2(m - top) : 0.f;
+          l += share * part_of(w)[kPartFloats + j];
+          acc += share * *reinterpret_cast<const f32x4*>(part_of(w) + j * kDims + ((ch ^ (j & 15)) << 2));
+        }
+        const float inv = l != 0.f ? 1.0f / l : 0.f;
+        store4<OutT>(out + at + half * kDims + 4 * ch, acc * inv);
+      }
+    }
+  }
+}
+
+struct PagedArgs {
+  const uint16_t *q, *k, *v;
+  PagedPlan plan;
+  void* out;
+  unsigned grid;
+  hipStream_t stream;
+};
+
+template <typename OutT, int kChange>
+void launch_change(const PagedArgs& a, bool split_kv) {
+  const dim3 grid(a.grid), block(64 * kWaves);
+  if (split_kv)
+    hipLaunchKernelGGL((prefill_paged_kernel<OutT, kChange, true>), grid, block, 0, a.stream, a.q, a.k, a.v, a.plan,
+                       static_cast<OutT*>(a.out));
+  else
+    hipLaunchKernelGGL((prefill_paged_kernel<OutT, kChange, false>), grid, block, 0, a.stream, a.q, a.k, a.v, a.plan,
+                       static_cast<OutT*>(a.out));
+}
+
+template <typename OutT>
+void launch_paged(const PagedArgs& a, int change, bool split_kv) {
+  if (change == kPlain) return launch_change<OutT, kPlain>(a, split_kv);
+  if (change == kBias) return launch_change<OutT, kBias>(a, split_kv);
+  if (change == kCap) return launch_change<OutT, kCap>(a, split_kv);
+  launch_change<OutT, kCapBias>(a, split_kv);
+}
+
+}  // namespace
+
+extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, const void* k_pages, const void* v_pages,
+                                          int32_t num_pages, const int32_t* block_tables, int32_t max_pages_per_seq,
+                                          const int32_t* seq_lens, const int32_t* q_starts, const int32_t* q_lens,
+                                          int32_t num_seqs, int32_t total_q, int32_t max_q_len, float scale,
+                                          const ctx_attn_scores* scores, void* out, void* stream) {
+  int rc = check_common(h, num_seqs, scale);
+  if (rc != CTX_OK) return rc;
+  ctx_attn_scores sc{};
+  if (scores != nullptr) sc = *scores;
+  rc = check_scored(h, sc, scale, num_pages, max_pages_per_seq);
+  if (rc != CTX_OK) return rc;
+  if (total_q < 0 || max_q_len < 0)
+    return fail(CTX_ERR_INVALID_ARG, "total_q and max_q_len must not be negative (%d, %d)", total_q, max_q_len);
+  if (num_seqs == 0 || max_q_len == 0 || total_q == 0) return CTX_OK;
+  if (q == nullptr || k_pages == nullptr || v_pages == nullptr || block_tables == nullptr || seq_lens == nullptr ||
+      q_starts == nullptr || q_lens == nullptr || out == nullptr)
+    return fail(CTX_ERR_INVALID_ARG, "NULL data pointer");
+  if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out))
+    return fail(CTX_ERR_ALIGNMENT, "q, k_pages, v_pages and out must be 16-byte aligned");
+  rc = check_device(h);
+  if (rc != CTX_OK) return rc;
+  const ctx_decode_attn_desc& d = h->desc;
+  const int g = d.num_q_heads / d.num_kv_heads;
+  const int tiles = d.out_dtype == CTX_DTYPE_F32 ? 2 : 3;  // 16-column tiles per wave
+  PagedPlan pp{};
+  pp.block_tables = block_tables;
+  pp.lens = seq_lens;
+  pp.q_starts = q_starts;
+  pp.q_lens = q_lens;
+  pp.prefix_lens = sc.prefix_lens;
+  pp.doc_starts = sc.doc_starts;
+  pp.slopes = sc.slopes;
+  pp.window = sc.window;
+  pp.max_pages = max_pages_per_seq;
+  pp.num_pages = num_pages;
+  pp.page_tokens = d.page_tokens;
+  pp.total_q = total_q;
+  pp.max_q_len = max_q_len < total_q ? max_q_len : total_q;
+  pp.hq = d.num_q_heads;
+  pp.hkv = d.num_kv_heads;
+  pp.group = g;
+  pp.units = num_seqs * d.num_kv_heads;
+  pp.factor = (float)((double)scale * 1.4426950408889634);
+  pp.cap_in = sc.softcap > 0.f ? scale / sc.softcap : 0.f;
+  pp.cap_in2 = (float)((double)pp.cap_in * 2.8853900817779268);
+  pp.cap_out = (float)((double)sc.softcap * 1.4426950408889634);
+  const int64_t cols = (int64_t)pp.max_q_len * g;
+  const int64_t units = round_up((int64_t)num_seqs * d.num_kv_heads, kXcds);  // whole XCD rounds
+  const auto grid_of = [&](int64_t wg_cols) { return units * ((cols + wg_cols - 1) / wg_cols); };
+  const int64_t wide = grid_of(kWaves * tiles * 16), narrow = grid_of(tiles * 16);
+  // Narrow workgroups as long as all of them are resident at once (two per CU), as in
+  // the contiguous prefill: in a second round each pays its start and its merge again.
+  const bool split_kv = narrow <= 2 * (int64_t)h->num_cus;
+  const int64_t blocks = split_kv ? narrow : wide;
+  if (blocks > INT32_MAX) return fail(CTX_ERR_INVALID_ARG, "prefill grid too large");
+  pp.tiles = (int32_t)(blocks / units);
+  pp.last_first = blocks > 2 * (int64_t)h->num_cus;
+  const PagedArgs a{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k_pages),
+                    static_cast<const uint16_t*>(v_pages), pp, out, (unsigned)blocks,
+                    reinterpret_cast<hipStream_t>(stream)};
+  const int change = (sc.softcap > 0.f ? kCap : kPlain) + (sc.slopes != nullptr ? kBias : kPlain);
+  if (d.out_dtype == CTX_DTYPE_F32)
+    launch_paged<float>(a, change, split_kv);
+  else
+    launch_paged<uint16_t>(a, change, split_kv);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return hip_fail(e, "kernel launch");
+  return CTX_OK;
+}

@@ -128,10 +128,13 @@ def seen_tokens(length, p, window=0, prefix=0, doc=0):
     return (t < prefix) | ((t >= low) & (t <= p))
 
 
-def attention_reference(bt: Batch, scale, softcap=0.0, window=0, slopes=None, prefix=None, docs=None, per_row=True):
+def attention_reference(bt: Batch, scale, softcap=0.0, window=0, slopes=None, prefix=None, docs=None, per_row=True,
+                        spread=False):
     """Outputs [rows, Hq, D] in 64 bits (NaN in rows of no sequence) of every packed row against bt's
-    caches; docs per packed row, or per sequence (per_row False)."""
+    caches; docs per packed row, or per sequence (per_row False).  spread: also the weighted mean of
+    |value - output|, which bounds what a relative error of the weights does to the output."""
     out = torch.full((bt.rows, bt.hq, D), float("nan"), dtype=torch.float64)
+    wide = torch.zeros_like(out)
     g = bt.hq // bt.hkv
     cache = {}
     for j, at in enumerate(bt.row_of()):
@@ -159,5 +162,10 @@ def attention_reference(bt: Batch, scale, softcap=0.0, window=0, slopes=None, pr
             s = softcap * torch.tanh(s / softcap)
         if slopes is not None:
             s = s - slopes.double().view(bt.hkv, g, 1) * (p - t).abs().double()
-        out[j] = torch.einsum("hgt,thd->hgd", torch.softmax(s, -1), vb[t]).reshape(bt.hq, D)
-    return out
+        w = torch.softmax(s, -1)
+        o = torch.einsum("hgt,thd->hgd", w, vb[t])
+        out[j] = o.reshape(bt.hq, D)
+        if spread:
+            far = (vb[t].permute(1, 0, 2)[:, None] - o[:, :, None]).abs()
+            wide[j] = (w[..., None] * far).sum(2).reshape(bt.hq, D)
+    return (out, wide) if spread else out
