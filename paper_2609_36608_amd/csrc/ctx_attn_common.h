@@ -165,7 +165,7 @@ int check_common(ctx_decode_attn* h, int32_t num_seqs, float scale) {
   return CTX_OK;
 }
 
-constexpr int32_t kMostTokens = 1 << 30;  // of a sequence in paged caches: positions stay in 32 bits
+constexpr int32_t kMostTokens = 1 << 30;  // in paged caches: rows and positions stay in 32 bits, with some to spare
 
 // Checks of what the calls over paged caches with changed scores share.
 [[maybe_unused]] int check_scored(const ctx_decode_attn* h, const ctx_attn_scores& sc, float scale,
@@ -173,8 +173,8 @@ constexpr int32_t kMostTokens = 1 << 30;  // of a sequence in paged caches: posi
   if (h->desc.page_tokens <= 0) return fail(CTX_ERR_UNSUPPORTED, "the handle was created without page_tokens");
   if (num_pages < 0 || max_pages <= 0)
     return fail(CTX_ERR_INVALID_ARG, "num_pages must not be negative and max_pages_per_seq must be positive");
-  if ((int64_t)num_pages * h->desc.page_tokens > INT32_MAX)
-    return fail(CTX_ERR_UNSUPPORTED, "caches of more than 2^31 - 1 tokens");
+  if ((int64_t)num_pages * h->desc.page_tokens > kMostTokens)
+    return fail(CTX_ERR_UNSUPPORTED, "caches of more than %d tokens", kMostTokens);
   if (!(std::isfinite(sc.softcap) && sc.softcap >= 0.f))
     return fail(CTX_ERR_INVALID_ARG, "softcap must be finite and >= 0");
   if (sc.softcap > 0.f && !std::isfinite(scale / sc.softcap))

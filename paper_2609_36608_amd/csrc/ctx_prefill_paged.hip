@@ -243,7 +243,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   // The maxima start at the largest bias of the column: where biases grow with the
   // distance, the first scores are rounded near it and not near 0.
   Softmax st[kTiles];
-  float limit[kTiles];  // relative scores above it move the maximum; -inf: there is none yet
+  int unset = (1 << kTiles) - 1;  // bit ct: the column has seen no token yet
   f32x4 o[kTiles][8];
 #pragma unroll
   for (int ct = 0; ct < kTiles; ++ct) {
@@ -253,52 +253,77 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
       const int ahead = prefix - 1 - last[ct];
       st[ct].m = -slope[ct] * (float)(back > ahead ? back : ahead);
     }
-    limit[ct] = -INFINITY;
 #pragma unroll
     for (int nb = 0; nb < 8; ++nb) o[ct][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // cache rows of the half blocks from flattened token `held` on, one per lane; -1: on no page
-  int held = 0, rows = -1;
+  // Of the kHeld half blocks from flattened token `held` on, one per lane: its first cache
+  // row / 16, whether it has tokens between prefix and `first` (kEdge), and its tokens
+  // that are seen at all; 0 outside the cache and past the end.
+  constexpr uint32_t kEdge = 32;
+  int held = 0;
+  uint32_t halves = 0;
   auto look_up = [&](int v) __attribute__((always_inline)) {
     held = v;
-    const int t = token(v + lane * kHalf);
-    rows = -1;
-    if (v + lane * kHalf < v_end && t < end) {
+    halves = 0;
+    const int at = v + lane * kHalf;
+    const int t = token(at);
+    if (at < v_end) {
       const int j = t / pp.page_tokens;
       if (j < pp.max_pages) {
         const int page = pp.block_tables[(size_t)b * pp.max_pages + j];
-        if (page >= 0 && page < pp.num_pages) rows = page * pp.page_tokens + (t - j * pp.page_tokens);
+        if (page >= 0 && page < pp.num_pages) {
+          const int row = page * pp.page_tokens + (t - j * pp.page_tokens);
+          const uint32_t edge = t < first && t + kHalf > prefix ? kEdge : 0u;
+          halves = (uint32_t)(row / kHalf) << 6 | edge | (uint32_t)(end - t < kHalf ? end - t : kHalf);
+        }
       }
     }
   };
   // A block load writes lane L's 16 bytes at LDS base + 16 L: round r of wave w fills
   // slots 0..15 of tokens (r kStagers + w) 4 + L / 16 of a half block, so each lane fetches
   // the chunk that the swizzle puts at its slot (the swizzle repeats every 16 tokens).
-  int offset[kRounds], lane_tok[kRounds];
+  int offset[kRounds];
 #pragma unroll
   for (int r = 0; r < kRounds; ++r) {
-    lane_tok[r] = (r * kStagers + stage_wave) * 4 + (lane >> 4);
-    offset[r] = lane_tok[r] * row_bytes + (((lane & 15) ^ tile_swizzle(lane_tok[r])) << 4);
+    const int tok = (r * kStagers + stage_wave) * 4 + (lane >> 4);
+    offset[r] = tok * row_bytes + (((lane & 15) ^ tile_swizzle(tok)) << 4);
   }
-  // Half h of the block at flattened token v, whose first cache row is `row`, into dst;
-  // outside the cache, past `end` and between prefix and `first` zeros are written.
-  auto load_half = [&](const uint16_t* base, int row, int v, int h, uint16_t* dst) __attribute__((always_inline)) {
-    const int t = token(v) + h * kHalf;
-    const int left = row < 0 ? 0 : end - t < kHalf ? end - t : kHalf;
-    const __amdgpu_buffer_rsrc_t rs =
-        make_rsrc(base + (row < 0 ? (size_t)0 : (size_t)row * row_elems), (uint32_t)((left < 0 ? 0 : left) * row_bytes));
-    const bool edge = t < first && t + kHalf > prefix;
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
-      int off = offset[r];
-      if (edge) off = t + lane_tok[r] >= prefix && t + lane_tok[r] < first ? kNowhere : off;
-      load16_to_lds(rs, dst + h * kHalf * kHeadDim + (r * kStagers + stage_wave) * 4 * kHeadDim, off);
-    }
+  // The words of the halves of the block at flattened token v, looked up if need be
+  struct Words {
+    uint32_t h[2];
   };
-  auto row_of = [&](int v, int h) {
-    const int i = (v - held) / kHalf + h;
-    return v < v_end ? __builtin_amdgcn_readlane(rows, i & (kHeld - 1)) : -1;
+  auto words_at = [&](int v) __attribute__((always_inline)) {
+    if (v - held >= kHeld * kHalf) look_up(v);
+    const int i = (int)((uint32_t)(v - held) / kHalf);
+    return Words{{(uint32_t)__builtin_amdgcn_readlane((int)halves, i), (uint32_t)__builtin_amdgcn_readlane((int)halves, i + 1)}};
+  };
+  auto absent_of = [](const Words& w) { return ((w.h[0] & 31) == 0 ? 1 : 0) | ((w.h[1] & 31) == 0 ? 2 : 0); };
+  // A block's loads, one instruction stream for every block (with a stream of its own for
+  // ordinary blocks the compiler lost count of the loads in flight and waited for all):
+  // outside the cache, past the end and between prefix and `first` zeros are written.
+  auto load_block = [&](const uint16_t* base, const Words& w, int v, uint16_t* dst) __attribute__((always_inline)) {
+    int off[2][kRounds];
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) off[0][r] = off[1][r] = offset[r];
+    if ((w.h[0] | w.h[1]) & kEdge) {
+      const int t = token(v);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+          const int x = t + h * kHalf + (r * kStagers + stage_wave) * 4 + (lane >> 4);
+          off[h][r] = (x >= prefix) & (x < first) ? kNowhere : offset[r];
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const __amdgpu_buffer_rsrc_t rs =
+          make_rsrc(base + (size_t)(w.h[h] >> 6) * (uint32_t)(kHalf * row_elems), (w.h[h] & 31) * (uint32_t)row_bytes);
+#pragma unroll
+      for (int r = 0; r < kRounds; ++r)
+        load16_to_lds(rs, dst + h * kHalf * kHeadDim + (r * kStagers + stage_wave) * 4 * kHeadDim, off[h][r]);
+    }
   };
 
   // per-lane LDS offsets of the operand reads within a 16-token half block
@@ -396,31 +421,34 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int t = t0 + 16 * h + 4 * c + i;
-            const bool see = (t < prefix || (t >= low[ct] && t <= last[ct])) && !(absent >> h & 1);
+            // no short circuits: they became branches around every score
+            const bool see = (int)((t < prefix) | ((t >= low[ct]) & (t <= last[ct]))) & ~(absent >> h);
             sc[ct][h][i] = see ? sc[ct][h][i] : -INFINITY;
           }
     }
   };
   // raises the maxima where a score passes its limit
   auto raise = [&](f32x4 (&sc)[kTiles][2]) __attribute__((always_inline)) {
+    // a score above the limit moves the maximum: 2^8 above it, or any where there is none
     float lm[kTiles];
     bool over = false;
 #pragma unroll
     for (int ct = 0; ct < kTiles; ++ct) {
       lm[ct] = max8(sc[ct][0], sc[ct][1]);
-      over = over || lm[ct] > limit[ct];
+      over |= lm[ct] > kHeadroom;
     }
-    if (!__any(over)) return;
+    if (!__any(over | (unset != 0))) return;
 #pragma unroll
     for (int ct = 0; ct < kTiles; ++ct) {
-      if (!__any(lm[ct] > limit[ct])) continue;
+      const bool fresh = unset >> ct & 1;
+      if (!__any(lm[ct] > (fresh ? -INFINITY : kHeadroom))) continue;
       const float top = column_max(lm[ct]);
-      const bool unset = limit[ct] < 0.f;
+      const bool none = fresh && !(top > -INFINITY);
       // what the rounded sum really moves by, so that a large maximum loses nothing
-      const float m = st[ct].m + (unset ? (top > -INFINITY ? top : 0.f) : fmaxf(top, 0.f));
+      const float m = st[ct].m + (none ? 0.f : fresh ? top : fmaxf(top, 0.f));
       const float delta = m - st[ct].m;
-      const float alpha = unset ? 1.f : fast_exp2(-delta);
-      limit[ct] = unset && !(top > -INFINITY) ? -INFINITY : kHeadroom;
+      const float alpha = fresh ? 1.f : fast_exp2(-delta);
+      if (!none) unset &= ~(1 << ct);
       st[ct].m = m;
       st[ct].l *= alpha;
 #pragma unroll
@@ -492,6 +520,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   auto any_seen = [&](int t0) { return t0 < prefix || (t0 <= some_last && t0 + kBlock > some_low); };
 
   look_up(0);
+  // The queries have arrived with the table's entries; said here, the compiler need not
+  // wait for them in the loop, where that would be a wait for the blocks in flight too.
+  __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
   if constexpr (!kSplitKv) {
     __shared__ __attribute__((aligned(16))) uint16_t lds_k1[kStageElems];
     __shared__ __attribute__((aligned(16))) uint16_t lds_v1[kStageElems];
@@ -499,14 +530,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     __shared__ __attribute__((aligned(16))) uint16_t lds_v2[kStageElems];
     int absent = 0;  // bits 2j, 2j + 1: of the block j steps on
     auto issue = [&](int v, uint16_t* dk, uint16_t* dv, int ahead) __attribute__((always_inline)) {
-      if (v < v_end && v - held >= kHeld * kHalf) look_up(v);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int row = row_of(v, h);
-        absent |= (row < 0 ? 1 : 0) << (2 * ahead + h);
-        load_half(khead, row, v, h, dk);
-        load_half(vhead, row, v, h, dv);
-      }
+      const Words w = words_at(v);
+      absent |= absent_of(w) << (2 * ahead);
+      load_block(khead, w, v, dk);
+      load_block(vhead, w, v, dv);
     };
     // One block: wait for this wave's loads of it, then the barrier (every wave's loads
     // have landed, and every wave is done with the stage read in the previous step); the
@@ -545,7 +572,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     for (int ct = 0; ct < kTiles; ++ct) {
       float l_tot = st[ct].l + __shfl_xor(st[ct].l, 16);
       l_tot += __shfl_xor(l_tot, 32);
-      const int64_t at = row_at((wave * kTiles + ct) * 16 + n);
+      // found anew: kept since the start, the rows took registers that the loop needs
+      int col = (wave * kTiles + ct) * 16 + n;
+      asm volatile("" : "+v"(col));
+      const int64_t at = row_at(col);
       if (at >= 0) {
         const float inv = l_tot != 0.f ? 1.0f / l_tot : 0.f;
         OutT* orow = out + at + 4 * c;
@@ -559,14 +589,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     constexpr int kStride = kWaves * kBlock;
     uint16_t* const kt = lds_k0 + wave * kBlockElems;
     uint16_t* const vt = lds_v0 + wave * kBlockElems;
-    auto fill = [&](const uint16_t* base, int v, uint16_t* dst) __attribute__((always_inline)) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) load_half(base, row_of(v, h), v, h, dst);
-    };
-    auto gone_at = [&](int v) { return (row_of(v, 0) < 0 ? 1 : 0) | (row_of(v, 1) < 0 ? 2 : 0); };
-    fill(khead, wave * kBlock, kt);
-    fill(vhead, wave * kBlock, vt);
-    int gone = gone_at(wave * kBlock);
+    Words w = words_at(wave * kBlock);
+    load_block(khead, w, wave * kBlock, kt);
+    load_block(vhead, w, wave * kBlock, vt);
     for (int v = wave * kBlock; v < v_end; v += kStride) {
       const int t0 = token(v);
       f32x4 sc[kTiles][2];
@@ -576,10 +601,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
       scores(kt, sc);
       // the tile's reads have returned before its refill is issued
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      const int next = v + kStride;
-      if (next < v_end && next - held >= kHeld * kHalf) look_up(next);
-      fill(khead, next, kt);
-      const int next_gone = gone_at(next);
+      const int gone = absent_of(w);
+      w = words_at(v + kStride);
+      load_block(khead, w, v + kStride, kt);
       relative(t0, gone, sc);
       raise(sc);
       weights(sc, pt);
@@ -587,8 +611,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
       asm volatile("" ::: "memory");
       values(vt, pt);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      fill(vhead, next, vt);
-      gone = next_gone;
+      load_block(vhead, w, v + kStride, vt);
     }
     __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
     __syncthreads();
@@ -610,7 +633,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
       l_tot += __shfl_xor(l_tot, 32);
       if (c == 0) {
         mine[kPartFloats + ct * 16 + n] = l_tot;
-        mine[kPartFloats + kCols + ct * 16 + n] = limit[ct] < 0.f ? -INFINITY : st[ct].m;
+        mine[kPartFloats + kCols + ct * 16 + n] = (unset >> ct & 1) ? -INFINITY : st[ct].m;
       }
     }
 #pragma unroll
