@@ -72,8 +72,9 @@ struct PagedPlan {
   int32_t total_q, max_q_len;
   int32_t hq, hkv, group;
   int32_t tiles;       // workgroups per (sequence, KV head)
+  int32_t num_seqs;
   int32_t units;       // sequences x KV heads
-  int32_t last_first;  // the tiles of a unit in falling order
+  int32_t last_first;  // the most work first
   float factor;        // of the product in log2 units, without a cap
   float cap_in, cap_in2, cap_out;  // scale / cap, twice that and cap in log2 units
 };
@@ -113,6 +114,29 @@ __device__ __forceinline__ int wave_extreme(int x) {
   return __builtin_amdgcn_readfirstlane(x);
 }
 
+// The sequence with k longer ones before it (in blocks of tokens; the first first where
+// they are equal), for up to 64: bit by bit of the length, from the top, the half of the
+// candidates that holds it.
+__device__ __forceinline__ int nth_longest(const int32_t* __restrict__ lens, int num_seqs, int k, int lane) {
+  constexpr int kBits = 16;
+  int len = lane < num_seqs ? lens[lane] : 0;
+  len = len < 0 ? 0 : len / kBlock < (1 << kBits) - 1 ? len / kBlock : (1 << kBits) - 1;
+  unsigned long long left = __ballot(lane < num_seqs);
+#pragma unroll
+  for (int bit = kBits - 1; bit >= 0; --bit) {
+    const unsigned long long ones = left & __ballot(len >> bit & 1);
+    const int n = __builtin_popcountll(ones);
+    if (k < n) {
+      left = ones;
+    } else {
+      k -= n;
+      left &= ~ones;
+    }
+  }
+  const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(left >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)left, 0u));
+  return __builtin_ctzll(__ballot((left >> lane & 1) && before == k));
+}
+
 template <typename OutT, int kChange, bool kSplitKv>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void prefill_paged_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ kc, const uint16_t* __restrict__ vc, PagedPlan pp,
@@ -134,14 +158,28 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   const int n = lane & 15;
   const int c = lane >> 4;
   const int g = pp.group;
-  // every tile of a unit on one XCD, whose L2 serves the tiles' re-reads; the last tile,
-  // which sees the most tokens, first where the grid is not resident at once
-  const int slot = blockIdx.x / kXcds;
-  const int tile = pp.last_first ? pp.tiles - 1 - slot % pp.tiles : slot % pp.tiles;
-  const int unit = (slot / pp.tiles) * kXcds + (int)(blockIdx.x % kXcds);
-  if (unit >= pp.units) return;
+  // Workgroups are dealt to the XCDs in turn.  Eight units at a time have one XCD each,
+  // whose L2 serves their tiles' re-reads; the tiles of the units left over (all of them,
+  // with fewer than 8) go to the XCDs in turn.  In a grid that is not resident at once the
+  // last tile, which sees the most tokens, goes first, and of up to 64 sequences the longest.
+  const int whole_units = pp.units & ~(kXcds - 1);
+  const int whole_blocks = whole_units * pp.tiles;
+  int tile, unit;
+  if ((int)blockIdx.x < whole_blocks) {
+    const int slot = blockIdx.x / kXcds;
+    tile = slot % pp.tiles;
+    unit = (slot / pp.tiles) * kXcds + (int)(blockIdx.x % kXcds);
+  } else {
+    const int at = (int)blockIdx.x - whole_blocks;
+    tile = at / (pp.units - whole_units);
+    unit = whole_units + at - tile * (pp.units - whole_units);
+  }
   const int kv = unit % pp.hkv;
-  const int b = unit / pp.hkv;
+  int b = unit / pp.hkv;
+  if (pp.last_first) {
+    tile = pp.tiles - 1 - tile;
+    if (pp.num_seqs <= 64) b = nth_longest(pp.lens, pp.num_seqs, b, lane);
+  }
   const int new_tokens = pp.q_lens[b];
   const int nq = new_tokens < pp.max_q_len ? new_tokens : pp.max_q_len;
   const int first_q = tile * kCols / g;
@@ -739,20 +777,21 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   pp.hq = d.num_q_heads;
   pp.hkv = d.num_kv_heads;
   pp.group = g;
+  pp.num_seqs = num_seqs;
   pp.units = num_seqs * d.num_kv_heads;
   pp.factor = (float)((double)scale * 1.4426950408889634);
   pp.cap_in = sc.softcap > 0.f ? scale / sc.softcap : 0.f;
   pp.cap_in2 = (float)((double)pp.cap_in * 2.8853900817779268);
   pp.cap_out = (float)((double)sc.softcap * 1.4426950408889634);
   const int64_t cols = (int64_t)pp.max_q_len * g;
-  const int64_t units = round_up((int64_t)num_seqs * d.num_kv_heads, kXcds);  // whole XCD rounds
+  const int64_t units = (int64_t)num_seqs * d.num_kv_heads;
   const auto grid_of = [&](int64_t wg_cols) { return units * ((cols + wg_cols - 1) / wg_cols); };
   const int64_t wide = grid_of(kWaves * tiles * 16), narrow = grid_of(tiles * 16);
   // Narrow workgroups as long as all of them are resident at once (two per CU), as in
   // the contiguous prefill: in a second round each pays its start and its merge again.
   const bool split_kv = narrow <= 2 * (int64_t)h->num_cus;
   const int64_t blocks = split_kv ? narrow : wide;
-  if (blocks > INT32_MAX) return fail(CTX_ERR_INVALID_ARG, "prefill grid too large");
+  if (units > INT32_MAX || blocks > INT32_MAX) return fail(CTX_ERR_INVALID_ARG, "prefill grid too large");
   pp.tiles = (int32_t)(blocks / units);
   pp.last_first = blocks > 2 * (int64_t)h->num_cus;
   const PagedArgs a{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k_pages),
