@@ -16,8 +16,8 @@
 // bf16 term of P; V^T through the LDS transpose read).
 //
 //   * Blocks: the tokens that some query of the workgroup sees are a prefix and a range
-//     further on.  Whole blocks between the two are passed over: the loop counts
-//     flattened tokens v, and token v + skip is meant from v = hole on.
+//     further on.  Whole blocks between the two are left out: tokens are numbered flattened,
+//     as v, and token v + skip is meant from v = hole on.
 //   * Pages: the cache rows of 64 half blocks (16 tokens, always within a page) are
 //     held one per lane, and looked up again when the loop has run past them.
 //   * Masks: a block that every column of the wave sees whole is not masked; one that
@@ -213,7 +213,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   float slope[kTiles];
   bf16x8 qb[kTiles][4];
   // over the wave's rows: what some row sees past the prefix, what all see
-  int some_low = INT_MAX, some_last = -1, all_low = INT_MIN, all_last = INT_MAX;
+  int some_low = INT_MAX, some_last = -1, all_low = 0, all_last = INT_MAX;
 #pragma unroll
   for (int ct = 0; ct < kTiles; ++ct) {
     const int col = (col_wave * kTiles + ct) * 16 + n;
@@ -277,6 +277,15 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   const int skip = first < until && (first & -kBlock) > hole ? (first & -kBlock) - hole : 0;
   const int v_end = end - skip;
   auto token = [&](int v) { return v < hole ? v : v + skip; };
+  // The wave's bounds in flattened tokens.  Tokens before the hole are the prefix's: no
+  // token past it is there unless skip is 0.
+  const int some_from = some_low - skip, some_to = some_last - skip;
+  const int all_from = all_low - skip, all_to = all_last - skip;
+  // Blocks are taken from the first on, with a bias from the last on: where scores
+  // fall with the distance, the maxima hardly move once the nearest block is done (steep
+  // heads raised them in every block).
+  const int blocks_end = (v_end + kBlock - 1) & -kBlock;
+  auto block_at = [&](int u) { return kHasBias ? blocks_end - kBlock - u : u; };
 
   // The maxima start at the largest bias of the column: where biases grow with the
   // distance, the first scores are rounded near it and not near 0.
@@ -295,18 +304,19 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     for (int nb = 0; nb < 8; ++nb) o[ct][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // Of the kHeld half blocks from flattened token `held` on, one per lane: its first cache
+  // Of the kHeld half blocks from the block at `held` of the order on, one per lane: its first cache
   // row / 16, whether it has tokens between prefix and `first` (kEdge), and its tokens
   // that are seen at all; 0 outside the cache and past the end.
   constexpr uint32_t kEdge = 32;
   int held = 0;
   uint32_t halves = 0;
-  auto look_up = [&](int v) __attribute__((always_inline)) {
-    held = v;
+  auto look_up = [&](int u) __attribute__((always_inline)) {
+    held = u;
     halves = 0;
-    const int at = v + lane * kHalf;
+    const int mine = u + (lane >> 1) * kBlock;
+    const int at = block_at(mine) + (lane & 1) * kHalf;
     const int t = token(at);
-    if (at < v_end) {
+    if (mine < blocks_end && at < v_end) {
       const int j = t / pp.page_tokens;
       if (j < pp.max_pages) {
         const int page = pp.block_tables[(size_t)b * pp.max_pages + j];
@@ -327,25 +337,28 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     const int tok = (r * kStagers + stage_wave) * 4 + (lane >> 4);
     offset[r] = tok * row_bytes + (((lane & 15) ^ tile_swizzle(tok)) << 4);
   }
-  // The words of the halves of the block at flattened token v, looked up if need be
+  // the words of the halves of the block at u of the order, looked up if need be
   struct Words {
     uint32_t h[2];
   };
-  auto words_at = [&](int v) __attribute__((always_inline)) {
-    if (v - held >= kHeld * kHalf) look_up(v);
-    const int i = (int)((uint32_t)(v - held) / kHalf);
+  auto words_at = [&](int u) __attribute__((always_inline)) {
+    if (u - held >= kHeld * kHalf) look_up(u);
+    const int i = (int)((uint32_t)(u - held) / kHalf);
     return Words{{(uint32_t)__builtin_amdgcn_readlane((int)halves, i), (uint32_t)__builtin_amdgcn_readlane((int)halves, i + 1)}};
   };
   auto absent_of = [](const Words& w) { return ((w.h[0] & 31) == 0 ? 1 : 0) | ((w.h[1] & 31) == 0 ? 2 : 0); };
   // A block's loads, one instruction stream for every block (with a stream of its own for
   // ordinary blocks the compiler lost count of the loads in flight and waited for all):
-  // outside the cache, past the end and between prefix and `first` zeros are written.
-  auto load_block = [&](const uint16_t* base, const Words& w, int v, uint16_t* dst) __attribute__((always_inline)) {
+  // outside the cache, past the end and, of values, between prefix and `first` zeros are
+  // written.  (Whatever keys give there is masked.)
+  auto load_block = [&](const uint16_t* base, bool values, const Words& w, int u, uint16_t* dst)
+      __attribute__((always_inline)) {
     int off[2][kRounds];
 #pragma unroll
     for (int r = 0; r < kRounds; ++r) off[0][r] = off[1][r] = offset[r];
-    if ((w.h[0] | w.h[1]) & kEdge) {
-      const int t = token(v);
+    if (values && ((w.h[0] | w.h[1]) & kEdge)) {
+      asm volatile("");  // a branch: not worked out for every block
+      const int t = token(block_at(u));
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -356,8 +369,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
+      const char* from = reinterpret_cast<const char*>(base) + (uint64_t)(w.h[h] >> 6) * (uint32_t)(kHalf * row_bytes);
       const __amdgpu_buffer_rsrc_t rs =
-          make_rsrc(base + (size_t)(w.h[h] >> 6) * (uint32_t)(kHalf * row_elems), (w.h[h] & 31) * (uint32_t)row_bytes);
+          make_rsrc(reinterpret_cast<const uint16_t*>(from), (w.h[h] & 31) * (uint32_t)row_bytes);
 #pragma unroll
       for (int r = 0; r < kRounds; ++r)
         load16_to_lds(rs, dst + h * kHalf * kHeadDim + (r * kStagers + stage_wave) * 4 * kHeadDim, off[h][r]);
@@ -389,11 +403,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
         for (int ct = 0; ct < kTiles; ++ct)
           sc[ct][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(kr[kk]), qb[ct][kk], sc[ct][h], 0, 0, 0);
     }
+    // no use of a product between the others: it would hold them up
+    __builtin_amdgcn_sched_barrier(0);
   };
 
   // The scores in log2 units less the running maxima, -inf where a token is not seen.
-  // t0: the block's first token; absent: bit h where half h is on no page.
-  auto relative = [&](int t0, int absent, f32x4 (&sc)[kTiles][2]) __attribute__((always_inline)) {
+  // v: the block's flattened token; whole: every column sees every token; absent: bit h
+  // where half h is on no page.
+  auto relative = [&](int v, bool whole, int absent, f32x4 (&sc)[kTiles][2]) __attribute__((always_inline)) {
     if constexpr (kHasCap && kTerms == 1) {
       // tanh(y) = 1 - 2 / (e^2y + 1): 2^-23 of the cap off, far below a bf16 weight's rounding
 #pragma unroll
@@ -426,7 +443,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     constexpr bool kTwoOver = kHasCap && kTerms == 1;
     const float factor = kTwoOver ? -2.0f * pp.cap_out : kHasCap ? pp.cap_out : pp.factor;
     const float shift = kTwoOver ? pp.cap_out : 0.f;
-    const bool whole = absent == 0 && (t0 + kBlock <= prefix || (t0 >= all_low && t0 + kBlock - 1 <= all_last));
+    const int t0 = token(v);
     const bool before = t0 + kBlock - 1 <= all_last;  // no token lies behind a query
     if (!kHasBias || before) {
 #pragma unroll
@@ -554,8 +571,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     }
     __builtin_amdgcn_s_setprio(0);
   };
-  // whether some row of the wave sees some token of the block at t0
-  auto any_seen = [&](int t0) { return t0 < prefix || (t0 <= some_last && t0 + kBlock > some_low); };
+  // the block at v whole: every column of the wave sees every token of it; some: any at all
+  auto is_whole = [&](int v, int absent) {
+    return absent == 0 && ((v >= all_from && v + kBlock - 1 <= all_to) || v + kBlock <= prefix);
+  };
+  auto is_some = [&](int v) { return v < prefix || (v <= some_to && v + kBlock > some_from); };
 
   look_up(0);
   // The queries have arrived with the table's entries; said here, the compiler need not
@@ -567,29 +587,29 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     __shared__ __attribute__((aligned(16))) uint16_t lds_k2[kStageElems];
     __shared__ __attribute__((aligned(16))) uint16_t lds_v2[kStageElems];
     int absent = 0;  // bits 2j, 2j + 1: of the block j steps on
-    auto issue = [&](int v, uint16_t* dk, uint16_t* dv, int ahead) __attribute__((always_inline)) {
-      const Words w = words_at(v);
+    auto issue = [&](int u, uint16_t* dk, uint16_t* dv, int ahead) __attribute__((always_inline)) {
+      const Words w = words_at(u);
       absent |= absent_of(w) << (2 * ahead);
-      load_block(khead, w, v, dk);
-      load_block(vhead, w, v, dv);
+      load_block(khead, false, w, u, dk);
+      load_block(vhead, true, w, u, dv);
     };
     // One block: wait for this wave's loads of it, then the barrier (every wave's loads
     // have landed, and every wave is done with the stage read in the previous step); the
     // loads of the block two ahead go into that stage.  The three stages are distinct LDS
     // arrays named at compile time, so the compiler's wait before the reads covers only
     // this stage's loads.
-    auto step = [&](int v, const uint16_t* kt, const uint16_t* vt, uint16_t* nk, uint16_t* nv) __attribute__((always_inline)) {
+    auto step = [&](int u, const uint16_t* kt, const uint16_t* vt, uint16_t* nk, uint16_t* nv) __attribute__((always_inline)) {
       __builtin_amdgcn_s_waitcnt(wait_vmcnt(2 * kLoads));
       lds_barrier();
       const int gone = absent & 3;
       absent >>= 2;
-      issue(v + 2 * kBlock, nk, nv, 1);
-      const int t0 = token(v);
-      if (v < v_end && any_seen(t0)) {
+      issue(u + 2 * kBlock, nk, nv, 1);
+      const int v = block_at(u);
+      if (u < blocks_end && is_some(v)) {
         f32x4 sc[kTiles][2];
         u32x4 pt[kTerms][kTiles];
         scores(kt, sc);
-        relative(t0, gone, sc);
+        relative(v, is_whole(v, gone), gone, sc);
         raise(sc);
         weights(sc, pt);
         values(vt, pt);
@@ -599,10 +619,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     issue(kBlock, lds_k1, lds_v1, 1);
     // whole rounds of three steps (an exit in the middle would make the compiler wait at
     // the loop's head); the last of them may be on empty blocks
-    for (int v = 0; v < v_end; v += 3 * kBlock) {
-      step(v, lds_k0, lds_v0, lds_k2, lds_v2);
-      step(v + kBlock, lds_k1, lds_v1, lds_k0, lds_v0);
-      step(v + 2 * kBlock, lds_k2, lds_v2, lds_k1, lds_v1);
+    for (int u = 0; u < blocks_end; u += 3 * kBlock) {
+      step(u, lds_k0, lds_v0, lds_k2, lds_v2);
+      step(u + kBlock, lds_k1, lds_v1, lds_k0, lds_v0);
+      step(u + 2 * kBlock, lds_k2, lds_v2, lds_k1, lds_v1);
     }
     // no load may land in LDS after the workgroup has released it
     __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
@@ -628,10 +648,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     uint16_t* const kt = lds_k0 + wave * kBlockElems;
     uint16_t* const vt = lds_v0 + wave * kBlockElems;
     Words w = words_at(wave * kBlock);
-    load_block(khead, w, wave * kBlock, kt);
-    load_block(vhead, w, wave * kBlock, vt);
-    for (int v = wave * kBlock; v < v_end; v += kStride) {
-      const int t0 = token(v);
+    load_block(khead, false, w, wave * kBlock, kt);
+    load_block(vhead, true, w, wave * kBlock, vt);
+    for (int u = wave * kBlock; u < blocks_end; u += kStride) {
+      const int v = block_at(u);
       f32x4 sc[kTiles][2];
       u32x4 pt[kTerms][kTiles];
       __builtin_amdgcn_s_waitcnt(wait_vmcnt(kLoads));  // this block's K; its V is still on the way
@@ -640,16 +660,16 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
       // the tile's reads have returned before its refill is issued
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       const int gone = absent_of(w);
-      w = words_at(v + kStride);
-      load_block(khead, w, v + kStride, kt);
-      relative(t0, gone, sc);
+      w = words_at(u + kStride);
+      load_block(khead, false, w, u + kStride, kt);
+      relative(v, is_whole(v, gone), gone, sc);
       raise(sc);
       weights(sc, pt);
       __builtin_amdgcn_s_waitcnt(wait_vmcnt(kLoads));  // this block's V
       asm volatile("" ::: "memory");
       values(vt, pt);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      load_block(vhead, w, v + kStride, vt);
+      load_block(vhead, true, w, u + kStride, vt);
     }
     __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
     __syncthreads();
@@ -778,7 +798,6 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   pp.hkv = d.num_kv_heads;
   pp.group = g;
   pp.num_seqs = num_seqs;
-  pp.units = num_seqs * d.num_kv_heads;
   pp.factor = (float)((double)scale * 1.4426950408889634);
   pp.cap_in = sc.softcap > 0.f ? scale / sc.softcap : 0.f;
   pp.cap_in2 = (float)((double)pp.cap_in * 2.8853900817779268);
@@ -792,6 +811,7 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   const bool split_kv = narrow <= 2 * (int64_t)h->num_cus;
   const int64_t blocks = split_kv ? narrow : wide;
   if (units > INT32_MAX || blocks > INT32_MAX) return fail(CTX_ERR_INVALID_ARG, "prefill grid too large");
+  pp.units = (int32_t)units;
   pp.tiles = (int32_t)(blocks / units);
   pp.last_first = blocks > 2 * (int64_t)h->num_cus;
   const PagedArgs a{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k_pages),
