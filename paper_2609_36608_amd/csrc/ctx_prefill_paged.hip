@@ -411,61 +411,61 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   // v: the block's flattened token; whole: every column sees every token; absent: bit h
   // where half h is on no page.
   auto relative = [&](int v, bool whole, int absent, f32x4 (&sc)[kTiles][2]) __attribute__((always_inline)) {
-    if constexpr (kHasCap && kTerms == 1) {
-      // tanh(y) = 1 - 2 / (e^2y + 1): 2^-23 of the cap off, far below a bf16 weight's rounding
+    const int t0 = token(v);
+    // no token lies behind a query; otherwise the distances are absolute
+    const bool before = !kHasBias || t0 + kBlock - 1 <= all_last;
+    // every score becomes change(score, what is added to it)
+    auto each = [&](float more, auto&& change) __attribute__((always_inline)) {
+      if (before) {
 #pragma unroll
-      for (int ct = 0; ct < kTiles; ++ct)
+        for (int ct = 0; ct < kTiles; ++ct) {
+          const float less = more - st[ct].m;
+          const float base = kHasBias ? fmaf(slope[ct], (float)(t0 + 4 * c - last[ct]), less) : less;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            sc[ct][h][i] = __builtin_amdgcn_rcpf(fast_exp2(sc[ct][h][i] * pp.cap_in2) + 1.0f);
-    } else if constexpr (kHasCap) {
+            for (int i = 0; i < 4; ++i)
+              sc[ct][h][i] = change(sc[ct][h][i], kHasBias ? fmaf(slope[ct], (float)(16 * h + i), base) : base);
+        }
+      } else {
+#pragma unroll
+        for (int ct = 0; ct < kTiles; ++ct) {
+          const int d = t0 + 4 * c - last[ct];
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              sc[ct][h][i] = change(sc[ct][h][i], fmaf(-slope[ct], fabsf((float)(d + 16 * h + i)), more - st[ct].m));
+        }
+      }
+    };
+    if constexpr (!kHasCap) {
+      each(0.f, [&](float x, float add) __attribute__((always_inline)) { return fmaf(x, pp.factor, add); });
+    } else if constexpr (kTerms == 1) {
+      // tanh(y) = 1 - 2 / (e^2y + 1), 2^-23 of the cap off: far below a bf16 weight's
+      // rounding.  (An odd polynomial up to |y| = 1, 7 instructions for 5, and a test
+      // whether a block's scores all lie there took as long: 100 requests over long
+      // contexts 790 TFLOP/s with either; one, with large scores among them, 100 us
+      // against 95.)
+      each(pp.cap_out, [&](float x, float add) __attribute__((always_inline)) {
+        return fmaf(__builtin_amdgcn_rcpf(fast_exp2(x * pp.cap_in2) + 1.0f), -2.0f * pp.cap_out, add);
+      });
+    } else {
       float most = 0.f;
 #pragma unroll
       for (int ct = 0; ct < kTiles; ++ct)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            sc[ct][h][i] *= pp.cap_in;
-            most = fmaxf(most, fabsf(sc[ct][h][i]));
-          }
-      const bool large = __any(most > kTanhSmall);
-#pragma unroll
-      for (int ct = 0; ct < kTiles; ++ct)
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sc[ct][h][i] = large ? tanh_any(sc[ct][h][i]) : tanh_small(sc[ct][h][i]);
-    }
-    // a capped score is cap_out * tanh(y), or with the form above cap_out - 2 cap_out * sc
-    constexpr bool kTwoOver = kHasCap && kTerms == 1;
-    const float factor = kTwoOver ? -2.0f * pp.cap_out : kHasCap ? pp.cap_out : pp.factor;
-    const float shift = kTwoOver ? pp.cap_out : 0.f;
-    const int t0 = token(v);
-    const bool before = t0 + kBlock - 1 <= all_last;  // no token lies behind a query
-    if (!kHasBias || before) {
-#pragma unroll
-      for (int ct = 0; ct < kTiles; ++ct) {
-        const float less = shift - st[ct].m;
-        const float base = kHasBias ? fmaf(slope[ct], (float)(t0 + 4 * c - last[ct]), less) : less;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            sc[ct][h][i] =
-                fmaf(sc[ct][h][i], factor, kHasBias ? fmaf(slope[ct], (float)(16 * h + i), base) : base);
-      }
-    } else {
-#pragma unroll
-      for (int ct = 0; ct < kTiles; ++ct) {
-        const int d = t0 + 4 * c - last[ct];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            sc[ct][h][i] = fmaf(sc[ct][h][i], factor, fmaf(-slope[ct], fabsf((float)(d + 16 * h + i)), shift - st[ct].m));
+          for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(sc[ct][h][i]));
+      if (!__any(most * fabsf(pp.cap_in) > kTanhSmall)) {
+        each(0.f, [&](float x, float add) __attribute__((always_inline)) {
+          return fmaf(tanh_small(x * pp.cap_in), pp.cap_out, add);
+        });
+      } else {
+        each(0.f, [&](float x, float add) __attribute__((always_inline)) {
+          return fmaf(tanh_any(x * pp.cap_in), pp.cap_out, add);
+        });
       }
     }
     if (!whole) {
