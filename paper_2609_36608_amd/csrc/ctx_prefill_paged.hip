@@ -18,8 +18,9 @@
 //   * Blocks: the tokens that some query of the workgroup sees are a prefix and a range
 //     further on.  Whole blocks between the two are left out: tokens are numbered flattened,
 //     as v, and token v + skip is meant from v = hole on.
-//   * Pages: the cache rows of 64 half blocks (16 tokens, always within a page) are
-//     held one per lane, and looked up again when the loop has run past them.
+//   * Pages: the cache rows of a wave's next 64 half blocks (16 tokens, always within a
+//     page) are held one per lane, and looked up again when the loop has run past them.
+//     (Asking for the next ones' pages a step ahead hid that wait and cost as much.)
 //   * Masks: a block that every column of the wave sees whole is not masked; one that
 //     none sees is passed over by the wave; tokens that no query of the workgroup sees
 //     are loaded as zeros, whatever the pages hold there.
@@ -304,16 +305,18 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     for (int nb = 0; nb < 8; ++nb) o[ct][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // Of the kHeld half blocks from the block at `held` of the order on, one per lane: its first cache
+  // Of the halves of the wave's next kHeld / 2 blocks, from `held` of the order on, one per
+  // lane: its first cache
   // row / 16, whether it has tokens between prefix and `first` (kEdge), and its tokens
   // that are seen at all; 0 outside the cache and past the end.
   constexpr uint32_t kEdge = 32;
+  constexpr int kStep = kSplitKv ? kWaves * kBlock : kBlock;  // between a wave's blocks
   int held = 0;
   uint32_t halves = 0;
   auto look_up = [&](int u) __attribute__((always_inline)) {
     held = u;
     halves = 0;
-    const int mine = u + (lane >> 1) * kBlock;
+    const int mine = u + (lane >> 1) * kStep;
     const int at = block_at(mine) + (lane & 1) * kHalf;
     const int t = token(at);
     if (mine < blocks_end && at < v_end) {
@@ -342,8 +345,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     uint32_t h[2];
   };
   auto words_at = [&](int u) __attribute__((always_inline)) {
-    if (u - held >= kHeld * kHalf) look_up(u);
-    const int i = (int)((uint32_t)(u - held) / kHalf);
+    if (u - held >= kHeld / 2 * kStep) look_up(u);
+    const int i = (int)((uint32_t)(u - held) / (kStep / 2));
     return Words{{(uint32_t)__builtin_amdgcn_readlane((int)halves, i), (uint32_t)__builtin_amdgcn_readlane((int)halves, i + 1)}};
   };
   auto absent_of = [](const Words& w) { return ((w.h[0] & 31) == 0 ? 1 : 0) | ((w.h[1] & 31) == 0 ? 2 : 0); };
@@ -577,7 +580,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   };
   auto is_some = [&](int v) { return v < prefix || (v <= some_to && v + kBlock > some_from); };
 
-  look_up(0);
+  const int u0 = kSplitKv ? wave * kBlock : 0;  // this wave's first block
+  look_up(u0);
   // The queries have arrived with the table's entries; said here, the compiler need not
   // wait for them in the loop, where that would be a wait for the blocks in flight too.
   __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
@@ -644,13 +648,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   } else {
     // Wave w takes blocks w, w + 4, w + 8, ... through its own K and V tiles.  A tile is
     // refilled with the wave's next block as soon as it has been read.
-    constexpr int kStride = kWaves * kBlock;
     uint16_t* const kt = lds_k0 + wave * kBlockElems;
     uint16_t* const vt = lds_v0 + wave * kBlockElems;
-    Words w = words_at(wave * kBlock);
-    load_block(khead, false, w, wave * kBlock, kt);
-    load_block(vhead, true, w, wave * kBlock, vt);
-    for (int u = wave * kBlock; u < blocks_end; u += kStride) {
+    Words w = words_at(u0);
+    load_block(khead, false, w, u0, kt);
+    load_block(vhead, true, w, u0, vt);
+    for (int u = u0; u < blocks_end; u += kStep) {
       const int v = block_at(u);
       f32x4 sc[kTiles][2];
       u32x4 pt[kTerms][kTiles];
@@ -660,8 +663,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
       // the tile's reads have returned before its refill is issued
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       const int gone = absent_of(w);
-      w = words_at(u + kStride);
-      load_block(khead, false, w, u + kStride, kt);
+      w = words_at(u + kStep);
+      load_block(khead, false, w, u + kStep, kt);
       relative(v, is_whole(v, gone), gone, sc);
       raise(sc);
       weights(sc, pt);
@@ -669,7 +672,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
       asm volatile("" ::: "memory");
       values(vt, pt);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      load_block(vhead, true, w, u + kStride, vt);
+      load_block(vhead, true, w, u + kStep, vt);
     }
     __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
     __syncthreads();
