@@ -128,6 +128,10 @@ typedef struct {
  * bf16 terms (24 significant bits).
  * Keys and values that some query of the sequence sees must be finite, their scores
  * too; what no query sees may hold anything.
+ * Calls with few rows share a long context out over workgroups that meet in the
+ * handle's workspace: as for ctx_decode_attn_run, calls that may overlap need separate
+ * handles.  num_seqs, total_q, max_q_len, the window, desc and the device's CU count choose the kernel; the
+ * same request alone and in a batch may differ by the rounding of its weights.
  * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, ALIGNMENT, HIP.
  */
 int ctx_prefill_attn_run_paged(ctx_decode_attn* handle, const void* q, const void* k_pages, const void* v_pages,

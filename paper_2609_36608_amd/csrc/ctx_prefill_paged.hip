@@ -51,7 +51,8 @@ namespace {
 constexpr int kLoadPolicy = 0;
 
 typedef __attribute__((address_space(3))) void lds_void;
-constexpr int kWaves = 4;
+constexpr int kWideWaves = 4;
+constexpr int wg_waves(int split) { return split > 0 ? split : kWideWaves; }
 constexpr int kBlock = 32;  // tokens
 constexpr int kHalf = 16;   // tokens of half a block: on one page
 constexpr int kBlockElems = kBlock * kHeadDim;
@@ -76,6 +77,9 @@ struct PagedPlan {
   int32_t num_seqs;
   int32_t units;       // sequences x KV heads
   int32_t last_first;  // the most work first
+  int32_t splits;      // workgroups that share the blocks of a tile; with more than one their
+  float* o_ws;         // partial outputs [splits, total_q, hq, D] and
+  float2* ml_ws;       // (maximum, sum) pairs go to the workspace
   float factor;        // of the product in log2 units, without a cap
   float cap_in, cap_in2, cap_out;  // scale / cap, twice that and cap in log2 units
 };
@@ -138,10 +142,13 @@ __device__ __forceinline__ int nth_longest(const int32_t* __restrict__ lens, int
   return __builtin_ctzll(__ballot((left >> lane & 1) && before == k));
 }
 
-template <typename OutT, int kChange, bool kSplitKv>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))) void prefill_paged_kernel(
+// kSplit: 0 for wide workgroups, or the waves of a narrow one.
+template <typename OutT, int kChange, int kSplit>
+__global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_per_eu(2))) void prefill_paged_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ kc, const uint16_t* __restrict__ vc, PagedPlan pp,
     OutT* __restrict__ out) {
+  constexpr bool kSplitKv = kSplit > 0;
+  constexpr int kWaves = wg_waves(kSplit);
   constexpr bool kHasBias = kChange == kBias || kChange == kCapBias;
   constexpr bool kHasCap = kChange == kCap || kChange == kCapBias;
   constexpr int kTerms = sizeof(OutT) == 4 ? 3 : 1;
@@ -166,12 +173,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   const int whole_units = pp.units & ~(kXcds - 1);
   const int whole_blocks = whole_units * pp.tiles;
   int tile, unit;
-  if ((int)blockIdx.x < whole_blocks) {
-    const int slot = blockIdx.x / kXcds;
+  const int share = pp.splits > 1 ? (int)blockIdx.x / (pp.tiles * pp.units) : 0;  // of the blocks
+  const int block = (int)blockIdx.x - share * (pp.tiles * pp.units);
+  if (block < whole_blocks) {
+    const int slot = block / kXcds;
     tile = slot % pp.tiles;
-    unit = (slot / pp.tiles) * kXcds + (int)(blockIdx.x % kXcds);
+    unit = (slot / pp.tiles) * kXcds + block % kXcds;
   } else {
-    const int at = (int)blockIdx.x - whole_blocks;
+    const int at = block - whole_blocks;
     tile = at / (pp.units - whole_units);
     unit = whole_units + at - tile * (pp.units - whole_units);
   }
@@ -286,6 +295,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   // fall with the distance, the maxima hardly move once the nearest block is done (steep
   // heads raised them in every block).
   const int blocks_end = (v_end + kBlock - 1) & -kBlock;
+  // this workgroup's share of them
+  const int per_share = pp.splits > 1 ? (blocks_end / kBlock + pp.splits - 1) / pp.splits * kBlock : blocks_end;
+  const int share_from = share * per_share;
+  const int share_end = share_from + per_share < blocks_end ? share_from + per_share : blocks_end;
   auto block_at = [&](int u) { return kHasBias ? blocks_end - kBlock - u : u; };
 
   // The maxima start at the largest bias of the column: where biases grow with the
@@ -319,7 +332,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     const int mine = u + (lane >> 1) * kStep;
     const int at = block_at(mine) + (lane & 1) * kHalf;
     const int t = token(at);
-    if (mine < blocks_end && at < v_end) {
+    if (mine < share_end && at < v_end) {
       const int j = t / pp.page_tokens;
       if (j < pp.max_pages) {
         const int page = pp.block_tables[(size_t)b * pp.max_pages + j];
@@ -580,7 +593,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
   };
   auto is_some = [&](int v) { return v < prefix || (v <= some_to && v + kBlock > some_from); };
 
-  const int u0 = kSplitKv ? wave * kBlock : 0;  // this wave's first block
+  const int u0 = share_from + (kSplitKv ? wave * kBlock : 0);  // this wave's first block
   look_up(u0);
   // The queries have arrived with the table's entries; said here, the compiler need not
   // wait for them in the loop, where that would be a wait for the blocks in flight too.
@@ -653,7 +666,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     Words w = words_at(u0);
     load_block(khead, false, w, u0, kt);
     load_block(vhead, true, w, u0, vt);
-    for (int u = u0; u < blocks_end; u += kStep) {
+    for (int u = u0; u < share_end; u += kStep) {
       const int v = block_at(u);
       f32x4 sc[kTiles][2];
       u32x4 pt[kTerms][kTiles];
@@ -685,7 +698,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
     static_assert((kPartFloats + 2 * kCols) * 4 <= 2 * kBlockElems * 2,
                   "a wave's partial results must fit half of a tile array");
     auto part_of = [&](int w) {
-      return reinterpret_cast<float*>((w < 2 ? lds_k0 : lds_v0) + (w & 1) * 2 * kBlockElems);
+      constexpr int kPerArray = kWaves / 2;
+      return reinterpret_cast<float*>((w < kPerArray ? lds_k0 : lds_v0) + w % kPerArray * 2 * kBlockElems);
     };
     float* const mine = part_of(wave);
 #pragma unroll
@@ -723,11 +737,61 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2))
           l += share * part_of(w)[kPartFloats + j];
           acc += share * *reinterpret_cast<const f32x4*>(part_of(w) + j * kDims + ((ch ^ (j & 15)) << 2));
         }
-        const float inv = l != 0.f ? 1.0f / l : 0.f;
-        store4<OutT>(out + at + half * kDims + 4 * ch, acc * inv);
+        if (pp.splits > 1) {
+          const int64_t part = share * pp.total_q * (int64_t)pp.hq + at / kHeadDim;
+          *reinterpret_cast<f32x4*>(pp.o_ws + part * kHeadDim + half * kDims + 4 * ch) = acc;
+          if (half == 0 && ch == 0) pp.ml_ws[part] = make_float2(top, l);
+        } else {
+          const float inv = l != 0.f ? 1.0f / l : 0.f;
+          store4<OutT>(out + at + half * kDims + 4 * ch, acc * inv);
+        }
       }
     }
   }
+}
+
+// Joins the shares of a tile's blocks: one wave per (row, head), two dimensions per lane,
+// the shares' weights one per lane; in share order.
+constexpr int kJoinWaves = 4;
+
+template <typename OutT>
+__global__ __launch_bounds__(64 * kJoinWaves) void prefill_join_kernel(PagedPlan pp, OutT* __restrict__ out) {
+  const int lane = threadIdx.x & 63;
+  const int64_t part = (int64_t)blockIdx.x * kJoinWaves + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  if (part >= (int64_t)pp.total_q * pp.hq) return;
+  const int row = (int)(part / pp.hq);
+  bool live = false;  // rows of no sequence have no shares
+  for (int base = 0; base < pp.num_seqs && !live; base += 64) {
+    const int b = base + lane;
+    if (b < pp.num_seqs) {
+      const int64_t i = (int64_t)row - pp.q_starts[b];
+      live = i >= 0 && i < pp.q_lens[b] && i < pp.max_q_len;
+    }
+    live = __any(live);
+  }
+  if (!live) return;
+  const int64_t stride = (int64_t)pp.total_q * pp.hq;
+  const float2 ml = lane < pp.splits ? pp.ml_ws[part + lane * stride] : make_float2(-INFINITY, 0.f);
+  float top = ml.x, sum = ml.y;
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+  const float weight = ml.x > -INFINITY ? fast_exp2(ml.x - top) : 0.f;
+  sum *= weight;
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+  float a = 0.f, b = 0.f;
+#pragma unroll 8
+  for (int s = 0; s < pp.splits; ++s) {
+    const float2 o = *reinterpret_cast<const float2*>(pp.o_ws + (part + s * stride) * kHeadDim + 2 * lane);
+    const float w = __shfl(weight, s);
+    a = fmaf(w, o.x, a);
+    b = fmaf(w, o.y, b);
+  }
+  const float inv = sum != 0.f ? 1.0f / sum : 0.f;
+  if constexpr (sizeof(OutT) == 4)
+    *reinterpret_cast<float2*>(out + part * kHeadDim + 2 * lane) = make_float2(a * inv, b * inv);
+  else
+    *reinterpret_cast<uint32_t*>(out + part * kHeadDim + 2 * lane) = pack_bf16x2(a * inv, b * inv);
 }
 
 struct PagedArgs {
@@ -738,23 +802,34 @@ struct PagedArgs {
   hipStream_t stream;
 };
 
+template <typename OutT, int kChange, int kSplit>
+void launch_split(const PagedArgs& a) {
+  hipLaunchKernelGGL((prefill_paged_kernel<OutT, kChange, kSplit>), dim3(a.grid), dim3(64 * wg_waves(kSplit)), 0,
+                     a.stream, a.q, a.k, a.v, a.plan, static_cast<OutT*>(a.out));
+}
+
 template <typename OutT, int kChange>
-void launch_change(const PagedArgs& a, bool split_kv) {
-  const dim3 grid(a.grid), block(64 * kWaves);
-  if (split_kv)
-    hipLaunchKernelGGL((prefill_paged_kernel<OutT, kChange, true>), grid, block, 0, a.stream, a.q, a.k, a.v, a.plan,
-                       static_cast<OutT*>(a.out));
-  else
-    hipLaunchKernelGGL((prefill_paged_kernel<OutT, kChange, false>), grid, block, 0, a.stream, a.q, a.k, a.v, a.plan,
-                       static_cast<OutT*>(a.out));
+void launch_change(const PagedArgs& a, int split) {
+  if (split == 8) return launch_split<OutT, kChange, 8>(a);
+  if (split == 4) return launch_split<OutT, kChange, 4>(a);
+  launch_split<OutT, kChange, 0>(a);
 }
 
 template <typename OutT>
-void launch_paged(const PagedArgs& a, int change, bool split_kv) {
-  if (change == kPlain) return launch_change<OutT, kPlain>(a, split_kv);
-  if (change == kBias) return launch_change<OutT, kBias>(a, split_kv);
-  if (change == kCap) return launch_change<OutT, kCap>(a, split_kv);
-  launch_change<OutT, kCapBias>(a, split_kv);
+void launch_paged(const PagedArgs& a, int change, int split) {
+  if (change == kPlain)
+    launch_change<OutT, kPlain>(a, split);
+  else if (change == kBias)
+    launch_change<OutT, kBias>(a, split);
+  else if (change == kCap)
+    launch_change<OutT, kCap>(a, split);
+  else
+    launch_change<OutT, kCapBias>(a, split);
+  if (a.plan.splits > 1) {
+    const int64_t parts = (int64_t)a.plan.total_q * a.plan.hq;
+    hipLaunchKernelGGL((prefill_join_kernel<OutT>), dim3((unsigned)((parts + kJoinWaves - 1) / kJoinWaves)),
+                       dim3(64 * kJoinWaves), 0, a.stream, a.plan, static_cast<OutT*>(a.out));
+  }
 }
 
 }  // namespace
@@ -808,23 +883,40 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   const int64_t cols = (int64_t)pp.max_q_len * g;
   const int64_t units = (int64_t)num_seqs * d.num_kv_heads;
   const auto grid_of = [&](int64_t wg_cols) { return units * ((cols + wg_cols - 1) / wg_cols); };
-  const int64_t wide = grid_of(kWaves * tiles * 16), narrow = grid_of(tiles * 16);
-  // Narrow workgroups as long as all of them are resident at once (two per CU), as in
-  // the contiguous prefill: in a second round each pays its start and its merge again.
-  const bool split_kv = narrow <= 2 * (int64_t)h->num_cus;
-  const int64_t blocks = split_kv ? narrow : wide;
+  const int64_t wide = grid_of(kWideWaves * tiles * 16), narrow = grid_of(tiles * 16);
+  const int64_t cus = h->num_cus;
+  // Narrow workgroups as long as all of them are resident at once (two of 4 waves per
+  // CU), as in the contiguous prefill: in a second round each pays its start and its merge
+  // again.  With one per CU or fewer they have 8 waves, and where they are fewer than the
+  // CUs several share a tile's blocks, through the workspace and a second launch: as many
+  // as fit there, leave each a context of 512 tokens and the join a wave's lanes.
+  const int split = narrow <= cus ? 8 : narrow <= 2 * cus ? 4 : 0;
+  pp.splits = 1;
+  if (split == 8) {
+    const int64_t slots = h->max_ranges + d.max_batch;
+    int64_t context = d.max_seq_len;
+    if (sc.window > 0 && sc.prefix_lens == nullptr && sc.window + tiles * 16 < context) context = sc.window + tiles * 16;
+    int64_t most = cus / narrow;
+    most = slots / total_q < most ? slots / total_q : most;
+    most = context / 512 < most ? context / 512 : most;
+    most = most < 64 ? most : 64;
+    if (most > 1) pp.splits = (int32_t)most;
+  }
+  pp.o_ws = h->o_ws;
+  pp.ml_ws = h->ml_ws;
+  const int64_t blocks = split > 0 ? narrow * pp.splits : wide;
   if (units > INT32_MAX || blocks > INT32_MAX) return fail(CTX_ERR_INVALID_ARG, "prefill grid too large");
   pp.units = (int32_t)units;
-  pp.tiles = (int32_t)(blocks / units);
-  pp.last_first = blocks > 2 * (int64_t)h->num_cus;
+  pp.tiles = (int32_t)(blocks / pp.splits / units);
+  pp.last_first = split == 0 && blocks > 2 * cus;
   const PagedArgs a{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k_pages),
                     static_cast<const uint16_t*>(v_pages), pp, out, (unsigned)blocks,
                     reinterpret_cast<hipStream_t>(stream)};
   const int change = (sc.softcap > 0.f ? kCap : kPlain) + (sc.slopes != nullptr ? kBias : kPlain);
   if (d.out_dtype == CTX_DTYPE_F32)
-    launch_paged<float>(a, change, split_kv);
+    launch_paged<float>(a, change, split);
   else
-    launch_paged<uint16_t>(a, change, split_kv);
+    launch_paged<uint16_t>(a, change, split);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(e, "kernel launch");
   return CTX_OK;

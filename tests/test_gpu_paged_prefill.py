@@ -34,11 +34,11 @@ def up(t):
 
 
 def run(bt, softcap=0.0, window=0, slopes=None, prefix=None, docs=None, out_dtype=torch.float32, scale=SCALE,
-        max_q_len=None, scored=True):
+        max_q_len=None, scored=True, max_seq_len=None):
     buf = torch.full((bt.rows + 1, bt.hq, D), -777.0, dtype=out_dtype, device=dev())
     kc, vc = up(bt.k), up(bt.v)
-    with DecodeAttention(bt.hq, bt.hkv, len(bt.lens), max(max(bt.lens), 1), page_tokens=bt.page,
-                         out_dtype=out_dtype) as attn:
+    with DecodeAttention(bt.hq, bt.hkv, len(bt.lens), max_seq_len or max(max(bt.lens), 1),
+                         page_tokens=bt.page, out_dtype=out_dtype) as attn:
         attn.prefill_paged(up(bt.q), kc, vc, up_i32(bt.table), up_i32(bt.lens), up_i32(bt.starts), up_i32(bt.new),
                            max(bt.new) if max_q_len is None else max_q_len, scale, buf[:bt.rows],
                            scores=AttnScores(softcap, window, up(slopes), i32(prefix), i32(docs)) if scored else None)
@@ -63,8 +63,8 @@ def close(got, live, ref, spread, out_dtype, share=1.0):
     assert (err <= bound).all(), f"worst {err.max().item():.3e}"
 
 
-def check(bt, out_dtype=torch.float32, scale=SCALE, share=1.0, **kw):
-    got, live = run(bt, out_dtype=out_dtype, scale=scale, **kw)
+def check(bt, out_dtype=torch.float32, scale=SCALE, share=1.0, max_seq_len=None, **kw):
+    got, live = run(bt, out_dtype=out_dtype, scale=scale, max_seq_len=max_seq_len, **kw)
     ref, spread = attention_reference(bt, scale, spread=True, **kw)
     close(got, live, ref, spread, out_dtype, share)
     return got, live
@@ -221,6 +221,27 @@ def test_long_histories(hist, new):
     assert is_wide(bt) == (new == 400)
     check(bt, torch.bfloat16)
     check(bt, window=1100, prefix=[50, 70], softcap=8.0)
+
+
+@pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("kind", KINDS)
+def test_few_rows_over_contexts_shared_out(kind, out_dtype):
+    """Handles whose bound lets several workgroups share a context: long ones, ones of a single
+    block, empty ones, and rows of no sequence between them."""
+    bt = Batch(53, [3000, 5, 33, 700, 0, 1200], [3, 5, 1, 2, 0, 4], 16, 16, 8, gap=1)
+    kw = scores_of(kind, bt, np.random.default_rng(8))
+    if kind in ("window", "all"):
+        kw["window"] = 600
+    check(bt, out_dtype, max_seq_len=30000, **kw)
+
+
+def test_shared_out_with_few_heads_and_one_row():
+    for hq, hkv in ((1, 1), (16, 1), (12, 2)):
+        bt = Batch(59 + hq, [5000], [1], 48, hq, hkv)
+        check(bt, torch.bfloat16, max_seq_len=1 << 20)
+        check(bt, slopes=slopes_of(hq), prefix=[40], window=4000)
+        bt.table[0, 30:] = -1  # the later shares see nothing
+        check(bt, max_seq_len=1 << 20)
 
 
 def test_large_logits_and_a_zero_scale():
