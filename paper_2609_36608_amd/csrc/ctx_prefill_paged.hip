@@ -142,8 +142,8 @@ __device__ __forceinline__ int nth_longest(const int32_t* __restrict__ lens, int
   return __builtin_ctzll(__ballot((left >> lane & 1) && before == k));
 }
 
-// kSplit: 0 for wide workgroups, or the waves of a narrow one.
-template <typename OutT, int kChange, int kSplit>
+// kSplit: 0 for wide workgroups, or the waves of a narrow one.  kTiles: 16-column tiles per wave.
+template <typename OutT, int kChange, int kSplit, int kTiles>
 __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_per_eu(2))) void prefill_paged_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ kc, const uint16_t* __restrict__ vc, PagedPlan pp,
     OutT* __restrict__ out) {
@@ -152,7 +152,6 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
   constexpr bool kHasBias = kChange == kBias || kChange == kCapBias;
   constexpr bool kHasCap = kChange == kCap || kChange == kCapBias;
   constexpr int kTerms = sizeof(OutT) == 4 ? 3 : 1;
-  constexpr int kTiles = sizeof(OutT) == 4 ? 2 : 3;
   constexpr int kCols = (kSplitKv ? 1 : kWaves) * kTiles * 16;
   constexpr int kStagers = kSplitKv ? 1 : kWaves;  // waves that stage a block together
   constexpr int kRounds = kHalf / (4 * kStagers);  // loads per thread and half block
@@ -802,29 +801,35 @@ struct PagedArgs {
   hipStream_t stream;
 };
 
-template <typename OutT, int kChange, int kSplit>
+// most tiles per wave: with fp32 outputs three would not leave registers for the terms
+template <typename OutT>
+constexpr int kMostTiles = sizeof(OutT) == 4 ? 2 : 3;
+
+template <typename OutT, int kChange, int kSplit, int kTiles>
 void launch_split(const PagedArgs& a) {
-  hipLaunchKernelGGL((prefill_paged_kernel<OutT, kChange, kSplit>), dim3(a.grid), dim3(64 * wg_waves(kSplit)), 0,
-                     a.stream, a.q, a.k, a.v, a.plan, static_cast<OutT*>(a.out));
+  hipLaunchKernelGGL((prefill_paged_kernel<OutT, kChange, kSplit, kTiles>), dim3(a.grid), dim3(64 * wg_waves(kSplit)),
+                     0, a.stream, a.q, a.k, a.v, a.plan, static_cast<OutT*>(a.out));
 }
 
 template <typename OutT, int kChange>
-void launch_change(const PagedArgs& a, int split) {
-  if (split == 8) return launch_split<OutT, kChange, 8>(a);
-  if (split == 4) return launch_split<OutT, kChange, 4>(a);
-  launch_split<OutT, kChange, 0>(a);
+void launch_change(const PagedArgs& a, int split, int tiles) {
+  if (split == 8) return launch_split<OutT, kChange, 8, kMostTiles<OutT>>(a);
+  if (split == 4) return launch_split<OutT, kChange, 4, kMostTiles<OutT>>(a);
+  if (tiles == 1) return launch_split<OutT, kChange, 0, 1>(a);
+  if (tiles == 2) return launch_split<OutT, kChange, 0, 2>(a);
+  launch_split<OutT, kChange, 0, kMostTiles<OutT>>(a);
 }
 
 template <typename OutT>
-void launch_paged(const PagedArgs& a, int change, int split) {
+void launch_paged(const PagedArgs& a, int change, int split, int tiles) {
   if (change == kPlain)
-    launch_change<OutT, kPlain>(a, split);
+    launch_change<OutT, kPlain>(a, split, tiles);
   else if (change == kBias)
-    launch_change<OutT, kBias>(a, split);
+    launch_change<OutT, kBias>(a, split, tiles);
   else if (change == kCap)
-    launch_change<OutT, kCap>(a, split);
+    launch_change<OutT, kCap>(a, split, tiles);
   else
-    launch_change<OutT, kCapBias>(a, split);
+    launch_change<OutT, kCapBias>(a, split, tiles);
   if (a.plan.splits > 1) {
     const int64_t parts = (int64_t)a.plan.total_q * a.plan.hq;
     hipLaunchKernelGGL((prefill_join_kernel<OutT>), dim3((unsigned)((parts + kJoinWaves - 1) / kJoinWaves)),
@@ -857,7 +862,6 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   if (rc != CTX_OK) return rc;
   const ctx_decode_attn_desc& d = h->desc;
   const int g = d.num_q_heads / d.num_kv_heads;
-  const int tiles = d.out_dtype == CTX_DTYPE_F32 ? 2 : 3;  // 16-column tiles per wave
   PagedPlan pp{};
   pp.block_tables = block_tables;
   pp.lens = seq_lens;
@@ -883,19 +887,35 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   const int64_t cols = (int64_t)pp.max_q_len * g;
   const int64_t units = (int64_t)num_seqs * d.num_kv_heads;
   const auto grid_of = [&](int64_t wg_cols) { return units * ((cols + wg_cols - 1) / wg_cols); };
-  const int64_t wide = grid_of(kWideWaves * tiles * 16), narrow = grid_of(tiles * 16);
   const int64_t cus = h->num_cus;
+  // most tokens that a row can see, as far as the host knows
+  const int most_tiles = d.out_dtype == CTX_DTYPE_F32 ? kMostTiles<float> : kMostTiles<uint16_t>;
+  int64_t context = d.max_seq_len;
+  if (sc.window > 0 && sc.prefix_lens == nullptr && (int64_t)sc.window + most_tiles * 16 < context)
+    context = (int64_t)sc.window + most_tiles * 16;
   // Narrow workgroups as long as all of them are resident at once (two of 4 waves per
   // CU), as in the contiguous prefill: in a second round each pays its start and its merge
-  // again.  With one per CU or fewer they have 8 waves, and where they are fewer than the
-  // CUs several share a tile's blocks, through the workspace and a second launch: as many
-  // as fit there, leave each a context of 512 tokens and the join a wave's lanes.
-  const int split = narrow <= cus ? 8 : narrow <= 2 * cus ? 4 : 0;
+  // again.  With one per CU or fewer they have 8 waves: 256 new tokens over 4,000 34 us (4
+  // waves 42, wide 82).  Not for short contexts, which leave a wave few blocks: 400 fresh
+  // tokens 13.5 us wide, 15.8 narrow.
+  const int64_t narrow = grid_of(most_tiles * 16);
+  const int split = context <= 16 * kBlock || narrow > 2 * cus ? 0 : narrow > cus ? 4 : 8;
+  // Wide ones have fewer tiles per wave where there would be too few to fill the chip: one
+  // tile as long as all workgroups are resident (three per CU), two (of three) as long as
+  // about all are (two per CU).  Of 1, 2 and 3 tiles: 1,024 new tokens over 4,000 117, 124
+  // and 149 us, 2,048 248, 186 and 209, 4,096 484, 395 and 397; 8 requests with up to 120 over
+  // 600 24, 26 and 32, with up to 300 54, 59 and 46.
+  const auto wide = [&](int t) { return grid_of(kWideWaves * t * 16); };
+  const int tiles = split > 0             ? most_tiles
+                    : wide(1) <= 3 * cus ? 1
+                    : most_tiles > 2 && 4 * wide(2) <= 9 * cus ? 2
+                                                               : most_tiles;
+  // Where 8-wave workgroups are fewer than the CUs several share a tile's blocks, through
+  // the workspace and a second launch: as many as fit there, leave each a context of 512
+  // tokens and the join a wave's lanes.  16 new tokens over 20,000 30 us (142 alone).
   pp.splits = 1;
   if (split == 8) {
     const int64_t slots = h->max_ranges + d.max_batch;
-    int64_t context = d.max_seq_len;
-    if (sc.window > 0 && sc.prefix_lens == nullptr && sc.window + tiles * 16 < context) context = sc.window + tiles * 16;
     int64_t most = cus / narrow;
     most = slots / total_q < most ? slots / total_q : most;
     most = context / 512 < most ? context / 512 : most;
@@ -904,7 +924,7 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   }
   pp.o_ws = h->o_ws;
   pp.ml_ws = h->ml_ws;
-  const int64_t blocks = split > 0 ? narrow * pp.splits : wide;
+  const int64_t blocks = split > 0 ? narrow * pp.splits : wide(tiles);
   if (units > INT32_MAX || blocks > INT32_MAX) return fail(CTX_ERR_INVALID_ARG, "prefill grid too large");
   pp.units = (int32_t)units;
   pp.tiles = (int32_t)(blocks / pp.splits / units);
@@ -914,9 +934,9 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
                     reinterpret_cast<hipStream_t>(stream)};
   const int change = (sc.softcap > 0.f ? kCap : kPlain) + (sc.slopes != nullptr ? kBias : kPlain);
   if (d.out_dtype == CTX_DTYPE_F32)
-    launch_paged<float>(a, change, split);
+    launch_paged<float>(a, change, split, tiles);
   else
-    launch_paged<uint16_t>(a, change, split);
+    launch_paged<uint16_t>(a, change, split, tiles);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(e, "kernel launch");
   return CTX_OK;

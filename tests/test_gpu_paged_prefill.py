@@ -70,11 +70,37 @@ def check(bt, out_dtype=torch.float32, scale=SCALE, share=1.0, max_seq_len=None,
     return got, live
 
 
-def is_wide(bt, out_dtype=torch.bfloat16):
-    """Whether the call takes wide workgroups: more narrow ones than two per CU of 256."""
-    units = -(-len(bt.lens) * bt.hkv // 8) * 8
-    cols = 32 if out_dtype == torch.float32 else 48
-    return units * -(-max(bt.new) * (bt.hq // bt.hkv) // cols) > 512
+def kind_of(bt, out_dtype=torch.bfloat16, bound=None):
+    """The workgroups that the call takes on 256 CUs: ("wide", tiles per wave) or ("narrow", waves)."""
+    cols = max(bt.new) * (bt.hq // bt.hkv)
+    most = 2 if out_dtype == torch.float32 else 3
+    grid = lambda n: len(bt.lens) * bt.hkv * -(-cols // n)  # noqa: E731
+    narrow = grid(16 * most)
+    if (bound or max(bt.lens)) > 512 and narrow <= 512:
+        return "narrow", 8 if narrow <= 256 else 4
+    if grid(64) <= 768:
+        return "wide", 1
+    return "wide", 2 if most == 2 or grid(128) <= 576 else 3
+
+
+def kind_batch(kind, gap=1):
+    """A batch of 16 / 8 heads with odd and empty sequences that takes that kind with bf16 outputs,
+    and the bound of its handle."""
+    rng = np.random.default_rng(6)
+    if kind == "wide3":
+        new = rng.integers(1, 60, 40)
+        lens = new + rng.integers(0, 200, 40)
+        lens[:4], new[:4] = [300, 150, 33, 64], [300, 97, 33, 1]
+    elif kind == "narrow8":
+        lens, new = [150, 40, 0, 1, 300], [60, 40, 0, 1, 12]
+    else:
+        lens, new = [1, 40, 17, 33, 150, 300, 64, 0], [1, 40, 2, 1, 97, 12, 64, 0]
+        if kind == "wide2":
+            lens[4:6], new[4:6] = [480, 300], [450, 7]
+    bound = 600 if kind.startswith("narrow") else None
+    bt = Batch(3 + len(lens), lens, new, 16, 16, 8, gap=gap)
+    assert kind_of(bt, bound=bound) == (kind[:-1], int(kind[-1]))
+    return bt, bound
 
 
 def slopes_of(hq):
@@ -115,25 +141,13 @@ def scores_of(kind, bt, rng):
 
 
 @pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("kind", KINDS)
-def test_scores_and_masks_of_a_small_call(kind, out_dtype):
-    bt = Batch(3, LENS, NEW, 16, 16, 8, gap=2)
-    if kind == "cap":
+@pytest.mark.parametrize("scores", KINDS)
+@pytest.mark.parametrize("kind", ["wide1", "wide2", "wide3", "narrow4", "narrow8"])
+def test_scores_and_masks(kind, scores, out_dtype):
+    bt, bound = kind_batch(kind)
+    if scores == "cap":
         bt.q = randn(bt.g, bt.q.shape, 4.0)
-    check(bt, out_dtype, **scores_of(kind, bt, np.random.default_rng(4)))
-
-
-@pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("kind", KINDS)
-def test_scores_and_masks_of_a_call_that_fills_the_chip(kind, out_dtype):
-    """More narrow workgroups than are resident at once: wide ones."""
-    rng = np.random.default_rng(6)
-    new = rng.integers(1, 60, 40)
-    lens = new + rng.integers(0, 200, 40)
-    lens[:4], new[:4] = [300, 150, 33, 64], [300, 97, 33, 1]
-    bt = Batch(5, lens, new, 16, 16, 8, gap=1)
-    assert is_wide(bt)
-    check(bt, out_dtype, **scores_of(kind, bt, rng))
+    check(bt, out_dtype, max_seq_len=bound, **scores_of(scores, bt, np.random.default_rng(4)))
 
 
 @pytest.mark.parametrize("hq,hkv", [(32, 8), (28, 4), (16, 1), (5, 1), (9, 3), (7, 7), (30, 10), (1, 1)])
@@ -142,7 +156,7 @@ def test_heads_and_pages(hq, hkv, page):
     bt = Batch(hq + page, [1, page, page + 1, 3 * page + 7, 100], [1, page, 5, page + 30, 33], page, hq, hkv, gap=1)
     kw = dict(softcap=20.0, window=50, slopes=slopes_of(hq), prefix=[0, 3, page, 17, 40])
     check(bt, torch.bfloat16, **kw)
-    check(bt, torch.float32, **kw)
+    check(bt, torch.float32, max_seq_len=600, **kw)
 
 
 @pytest.mark.parametrize("window", [1, 2, 15, 16, 17, 31, 32, 33, 1000])
@@ -150,8 +164,8 @@ def test_heads_and_pages(hq, hkv, page):
 def test_window_edges(window, wide):
     lens, new = ([900, 90], [850, 3]) if wide else (LENS, NEW)
     bt = Batch(window, lens, new, 16, 16, 8)
-    assert is_wide(bt) == wide
-    check(bt, torch.bfloat16, window=window)
+    assert kind_of(bt, bound=900) == (("wide", 1) if wide else ("narrow", 4))
+    check(bt, torch.bfloat16, window=window, max_seq_len=900)
 
 
 @pytest.mark.parametrize("prefix", [0, 1, 31, 32, 33, 64, 65, 10 ** 6, -5])
@@ -159,8 +173,8 @@ def test_window_edges(window, wide):
 def test_prefix_edges(prefix, wide):
     lens, new = ([900, 90], [850, 80]) if wide else (LENS, NEW)
     bt = Batch(prefix & 255, lens, new, 16, 16, 8)
-    assert is_wide(bt) == wide
-    got, live = run(bt, window=20, prefix=[prefix] * len(lens))
+    assert kind_of(bt, torch.float32, bound=900) == (("wide", 1) if wide else ("narrow", 4))
+    got, live = run(bt, window=20, prefix=[prefix] * len(lens), max_seq_len=900)
     ref, spread = attention_reference(bt, SCALE, window=20, prefix=[min(max(prefix, 0), n) for n in lens], spread=True)
     close(got, live, ref, spread, torch.float32)
 
@@ -168,15 +182,16 @@ def test_prefix_edges(prefix, wide):
 @pytest.mark.parametrize("wide", [False, True])
 def test_rows_that_see_nothing_or_their_prefix_alone(wide):
     lens, new = ([900, 90, 50], [850, 90, 50]) if wide else ([100, 90, 50], [60, 90, 50])
-    bt = Batch(11, lens, new, 16, 8, 4)
-    assert is_wide(bt) == wide
+    bt = Batch(11, lens, new, 16, 16, 8)
+    kw = dict(max_seq_len=900)
+    assert kind_of(bt, bound=900) == (("wide", 1) if wide else ("narrow", 8))
     docs = np.full(bt.rows, 2 ** 31 - 1, np.int64)
-    got, live = run(bt, docs=docs)
+    got, live = run(bt, docs=docs, **kw)
     assert (got[live] == 0).all()
     docs[::2] = -7  # every other row sees all before it
-    check(bt, docs=docs)
-    check(bt, torch.bfloat16, docs=docs, prefix=[40, 0, 50], slopes=slopes_of(8) * 20)
-    check(bt, docs=docs, prefix=[3, 33, 1], slopes=slopes_of(8) * 20, softcap=9.0)
+    check(bt, docs=docs, **kw)
+    check(bt, torch.bfloat16, docs=docs, prefix=[40, 0, 50], slopes=slopes_of(16) * 20, **kw)
+    check(bt, docs=docs, prefix=[3, 33, 1], slopes=slopes_of(16) * 20, softcap=9.0, **kw)
 
 
 @pytest.mark.parametrize("wide", [False, True])
@@ -185,7 +200,7 @@ def test_unseen_slots_may_hold_anything(wide):
     oldest window, and in the slots behind the sequence (NaN in every test here)."""
     lens, new = ([1500, 300], [850, 2]) if wide else ([600, 300], [40, 2])
     bt = Batch(13, lens, new, 16, 16, 8)
-    assert is_wide(bt) == wide
+    assert kind_of(bt, torch.float32) == (("wide", 1) if wide else ("narrow", 8))
     kw = dict(window=45, prefix=[37, 3])
     clean, live = run(bt, **kw)
     for b, (n, m) in enumerate(zip(lens, new)):
@@ -200,17 +215,18 @@ def test_unseen_slots_may_hold_anything(wide):
 def test_pages_outside_the_cache_are_not_seen(wide):
     lens, new = ([700, 100, 90], [600, 50, 90]) if wide else ([200, 100, 90], [70, 50, 90])
     bt = Batch(17, lens, new, 16, 16, 8)
-    assert is_wide(bt) == wide
+    kw = dict(max_seq_len=900)
+    assert kind_of(bt, torch.float32, 900) == (("wide", 1) if wide else ("narrow", 8))
     bt.table[0, 3] = -1
     bt.table[0, 6] = bt.num_pages
     bt.table[1, :] = 2 ** 31 - 1  # nothing left
     bt.table[2, 0] = -2 ** 31
-    got, live = check(bt, softcap=30.0)
+    got, live = check(bt, softcap=30.0, **kw)
     rows = [j for j, at in enumerate(bt.row_of()) if at is not None and at[0] == 1]
     assert (got[rows] == 0).all()
-    check(bt, torch.bfloat16, window=60, prefix=[20, 0, 17])
+    check(bt, torch.bfloat16, window=60, prefix=[20, 0, 17], **kw)
     bt.table = np.ascontiguousarray(bt.table[:, :3])  # and tokens past the table
-    check(bt, slopes=slopes_of(16))
+    check(bt, slopes=slopes_of(16), **kw)
 
 
 @pytest.mark.parametrize("hist", [1000, 1024, 2100])
@@ -218,7 +234,7 @@ def test_pages_outside_the_cache_are_not_seen(wide):
 def test_long_histories(hist, new):
     """More half blocks than a wave holds cache rows for, in calls of both kinds."""
     bt = Batch(hist + new, [hist + new, 70], [new, 30], 16, 32, 8)
-    assert is_wide(bt) == (new == 400)
+    assert kind_of(bt) == (("wide", 1) if new == 400 else ("narrow", 8))
     check(bt, torch.bfloat16)
     check(bt, window=1100, prefix=[50, 70], softcap=8.0)
 
@@ -346,7 +362,7 @@ def test_graph_replays(wide):
 
     lens, new = ([900, 90], [850, 80]) if wide else ([300, 33], [60, 1])
     bt = Batch(47, lens, new, 16, 16, 8)
-    assert is_wide(bt) == wide
+    assert kind_of(bt, bound=900) == (("wide", 1) if wide else ("narrow", 8))
     q, kc, vc = up(bt.q), up(bt.k), up(bt.v)
     args = [up_i32(x) for x in (bt.table, bt.lens, bt.starts, bt.new)]
     sc = AttnScores(10.0, 50, up(slopes_of(16)), up_i32([5, 40]))
