@@ -109,13 +109,15 @@ __device__ __forceinline__ float column_max(float x) {
   return fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
 }
 
+// the least or largest over a row of 16 lanes, by rotations; the rows of a wave hold the
+// same columns
 template <bool kMin>
-__device__ __forceinline__ int wave_extreme(int x) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) {
-    const int y = __shfl_xor(x, off);
-    x = kMin ? (x < y ? x : y) : (x > y ? x : y);
-  }
+__device__ __forceinline__ int columns_extreme(int x) {
+  const auto with = [&](int y) { x = kMin ? (x < y ? x : y) : (x > y ? x : y); };
+  with(__builtin_amdgcn_mov_dpp(x, 0x128, 0xf, 0xf, false));
+  with(__builtin_amdgcn_mov_dpp(x, 0x124, 0xf, 0xf, false));
+  with(__builtin_amdgcn_mov_dpp(x, 0x122, 0xf, 0xf, false));
+  with(__builtin_amdgcn_mov_dpp(x, 0x121, 0xf, 0xf, false));
   return __builtin_amdgcn_readfirstlane(x);
 }
 
@@ -260,10 +262,10 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
       for (int kk = 0; kk < 4; ++kk) qb[ct][kk] = as_bf16x8(u32x4{0u, 0u, 0u, 0u});
     }
   }
-  some_low = wave_extreme<true>(some_low);
-  some_last = wave_extreme<false>(some_last);
-  all_low = wave_extreme<false>(all_low);
-  all_last = wave_extreme<true>(all_last);
+  some_low = columns_extreme<true>(some_low);
+  some_last = columns_extreme<false>(some_last);
+  all_low = columns_extreme<false>(all_low);
+  all_last = columns_extreme<true>(all_last);
   // the same over the workgroup: the tokens it reads
   int first = some_low, until = some_last + 1;
   if constexpr (!kSplitKv) {
