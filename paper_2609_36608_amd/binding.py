@@ -22,6 +22,7 @@ CTX_ERR_OOM = -6
 CTX_DTYPE_BF16 = 0
 CTX_DTYPE_F32 = 1
 
+HEAD_DIM = 128
 CTX_ROTARY_INTERLEAVED = 1  # ctx_rotary flag: pairs of neighbouring dimensions
 CTX_PREFILL_SPLIT_P = 1  # ctx_prefill_attn_run flag: softmax weights as two bf16 terms
 CTX_STATIC_SCRATCH_BYTES = 16 << 20  # static workspace of ctx_decode_attn_run_static, per device
@@ -208,6 +209,14 @@ def _check_tensors(device: int, checks) -> None:
             raise ValueError(f"{name} must be contiguous")
 
 
+def _need(name: str, t, dtype, device: int, shape) -> None:
+    """One contiguous tensor of that dtype and shape on cuda:device: four tests where nothing is wrong."""
+    if t.dtype is dtype and t.get_device() == device and t.is_contiguous() and t.shape == shape:
+        return
+    _check_tensors(device, ((name, t, dtype),))
+    raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+
+
 def _stream_ptr(stream, device=None) -> int:
     """hipStream_t of a torch stream (default: the current one of `device`) or a raw handle."""
     import torch
@@ -250,19 +259,20 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _scores_struct(scores: AttnScores, device: int, num_q_heads: int, seqs: int, rows: int) -> CtxAttnScores:
+def _scores_struct(scores: AttnScores, device: int, num_q_heads: int, seqs: int, rows: int):
+    """ctx_attn_scores of checked tensors, for a call (None: NULL)."""
     import torch
 
-    for name, t, dt, n in (("slopes", scores.slopes, torch.float32, num_q_heads),
-                           ("prefix_lens", scores.prefix_lens, torch.int32, seqs),
-                           ("doc_starts", scores.doc_starts, torch.int32, rows)):
-        if t is None:
-            continue
-        _check_tensors(device, ((name, t, dt),))
-        if t.shape != (n,):
-            raise ValueError(f"{name} must be [{n}]")
-    return CtxAttnScores(float(scores.softcap), int(scores.window), _ptr(scores.slopes), _ptr(scores.prefix_lens),
-                         _ptr(scores.doc_starts))
+    if scores is None:
+        return None
+    slopes, prefix, docs = scores.slopes, scores.prefix_lens, scores.doc_starts
+    if slopes is not None:
+        _need("slopes", slopes, torch.float32, device, (num_q_heads,))
+    if prefix is not None:
+        _need("prefix_lens", prefix, torch.int32, device, (seqs,))
+    if docs is not None:
+        _need("doc_starts", docs, torch.int32, device, (rows,))
+    return ctypes.byref(CtxAttnScores(scores.softcap, scores.window, _ptr(slopes), _ptr(prefix), _ptr(docs)))
 
 
 class DecodeAttention:
@@ -283,6 +293,7 @@ class DecodeAttention:
             raise error_for(self.lib, rc)
         self.handle = handle
         self.device = torch.cuda.current_device()
+        self.q_heads, self.kv_heads, self.page_tokens = num_q_heads, num_kv_heads, page_tokens
 
     def run(self, q, k_cache, v_cache, seq_offsets, seq_lens, scale: float, out, stream=None):
         import torch
@@ -318,11 +329,24 @@ class DecodeAttention:
 
         if self.handle is None:
             raise RuntimeError("handle is closed")
-        d = self.desc
         if (k_new is None) != (v_new is None):
             raise ValueError("k_new and v_new go together")
-        if scores is not None and k_new is not None:
-            raise ValueError("with scores, append the new tokens first (append_paged)")
+        if scores is not None:
+            if k_new is not None:
+                raise ValueError("with scores, append the new tokens first (append_paged)")
+            dev, b = self.device, q.shape[0]
+            _need("q", q, torch.bfloat16, dev, (b, self.q_heads, HEAD_DIM))
+            _need("out", out, self.out_dtype, dev, (b, self.q_heads, HEAD_DIM))
+            _need("seq_lens", seq_lens, torch.int32, dev, (b,))
+            self._check_pages(k_pages, v_pages, block_tables, b)
+            rc = self.lib.ctx_decode_attn_run_paged_scored(
+                self.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), k_pages.shape[0],
+                block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(), b, scale,
+                _scores_struct(scores, dev, self.q_heads, b, b), out.data_ptr(), _stream_ptr(stream))
+            if rc != CTX_OK:
+                raise error_for(self.lib, rc)
+            return out
+        d = self.desc
         checks = [("q", q, torch.bfloat16), ("k_pages", k_pages, torch.bfloat16),
                   ("v_pages", v_pages, torch.bfloat16), ("block_tables", block_tables, torch.int32),
                   ("seq_lens", seq_lens, torch.int32), ("out", out, self.out_dtype)]
@@ -340,14 +364,6 @@ class DecodeAttention:
         if k_new is not None and (k_new.shape != (b, d.num_kv_heads, d.head_dim) or v_new.shape != k_new.shape):
             raise ValueError(f"k_new/v_new must be [{b}, {d.num_kv_heads}, {d.head_dim}]")
         sp = _stream_ptr(stream)
-        if scores is not None:
-            rc = self.lib.ctx_decode_attn_run_paged_scored(
-                self.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), k_pages.shape[0],
-                block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(), b, float(scale),
-                ctypes.byref(_scores_struct(scores, self.device, d.num_q_heads, b, b)), out.data_ptr(), sp)
-            if rc != CTX_OK:
-                raise error_for(self.lib, rc)
-            return out
         rc = self.lib.ctx_decode_attn_run_paged(
             self.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), block_tables.data_ptr(),
             block_tables.shape[1], seq_lens.data_ptr(), b,
@@ -360,14 +376,25 @@ class DecodeAttention:
     def _check_pages(self, k_pages, v_pages, block_tables, seqs: int):
         import torch
 
-        d = self.desc
-        _check_tensors(self.device, (("k_pages", k_pages, torch.bfloat16), ("v_pages", v_pages, torch.bfloat16),
-                                     ("block_tables", block_tables, torch.int32)))
-        if k_pages.dim() != 4 or k_pages.shape[1:] != (d.page_tokens, d.num_kv_heads, d.head_dim) \
-                or v_pages.shape != k_pages.shape:
-            raise ValueError(f"k_pages/v_pages must be [pages, {d.page_tokens}, {d.num_kv_heads}, {d.head_dim}]")
-        if block_tables.dim() != 2 or block_tables.shape[0] != seqs:
-            raise ValueError(f"block_tables must be [{seqs}, max_pages]")
+        pages = (k_pages.shape[0], self.page_tokens, self.kv_heads, HEAD_DIM)
+        _need("k_pages", k_pages, torch.bfloat16, self.device, pages)
+        _need("v_pages", v_pages, torch.bfloat16, self.device, pages)
+        _need("block_tables", block_tables, torch.int32, self.device, (seqs, block_tables.shape[-1]))
+
+    def _row_stride(self, name: str, t, rows: int, heads: int) -> int:
+        """Elements between the rows of heads that may be slices of wider rows."""
+        import torch
+
+        if t.dtype is not torch.bfloat16:
+            raise TypeError(f"{name} must be torch.bfloat16, got {t.dtype}")
+        if t.get_device() != self.device:
+            raise ValueError(f"{name} must be on cuda:{self.device}")
+        if t.shape != (rows, heads, HEAD_DIM):
+            raise ValueError(f"{name} must be [{rows}, {heads}, {HEAD_DIM}]")
+        row, head, dim = t.stride()
+        if dim != 1 or (head != HEAD_DIM and heads > 1):
+            raise ValueError(f"the heads of {name} must be contiguous within its rows")
+        return row if rows > 1 else heads * HEAD_DIM  # the stride of a single row says nothing
 
     def append_paged(self, k, v, k_pages, v_pages, block_tables, seq_lens, q=None, q_out=None, q_starts=None,
                      q_lens=None, rotary: Rotary | None = None, stream=None):
@@ -380,61 +407,44 @@ class DecodeAttention:
 
         if self.handle is None:
             raise RuntimeError("handle is closed")
-        d = self.desc
-        if q is None and q_out is not None:
-            raise ValueError("q_out needs q")
         if (q_starts is None) != (q_lens is None):
             raise ValueError("q_starts and q_lens go together")
-        rows, seqs = k.shape[0], seq_lens.shape[0]
-        strides = []
-        for name, t, heads in (("q", q, d.num_q_heads), ("k", k, d.num_kv_heads), ("v", v, d.num_kv_heads)):
-            if t is None:
-                strides.append(0)
-                continue
-            if t.dtype != torch.bfloat16:
-                raise TypeError(f"{name} must be torch.bfloat16, got {t.dtype}")
-            if not t.is_cuda or t.device.index != self.device:
-                raise ValueError(f"{name} must be on cuda:{self.device}")
-            if t.shape != (rows, heads, d.head_dim):
-                raise ValueError(f"{name} must be [{rows}, {heads}, {d.head_dim}]")
-            if (heads > 1 and t.stride(1) != d.head_dim) or t.stride(2) != 1:
-                raise ValueError(f"the heads of {name} must be contiguous within its rows")
-            # the stride of a single row says nothing
-            strides.append(t.stride(0) if rows > 1 else heads * d.head_dim)
-        self._check_pages(k_pages, v_pages, block_tables, seqs)
-        _check_tensors(self.device, (("seq_lens", seq_lens, torch.int32),))
-        if q_starts is not None:
-            _check_tensors(self.device, (("q_starts", q_starts, torch.int32), ("q_lens", q_lens, torch.int32)))
-            if q_starts.shape != (seqs,) or q_lens.shape != (seqs,) or seq_lens.shape != (seqs,):
-                raise ValueError(f"q_starts, q_lens, seq_lens must all be [{seqs}]")
-        elif seq_lens.shape != (rows,):
-            raise ValueError(f"without q_starts, seq_lens must be [{rows}]")
+        dev, rows, seqs = self.device, k.shape[0], seq_lens.shape[0]
+        k_stride, v_stride = self._row_stride("k", k, rows, self.kv_heads), self._row_stride("v", v, rows, self.kv_heads)
+        q_stride = 0
         if q is not None:
+            q_stride = self._row_stride("q", q, rows, self.q_heads)
             if q_out is None:
-                q_out = torch.empty((rows, d.num_q_heads, d.head_dim), dtype=torch.bfloat16, device=q.device)
-            _check_tensors(self.device, (("q_out", q_out, torch.bfloat16),))
-            if q_out.shape != (rows, d.num_q_heads, d.head_dim):
-                raise ValueError(f"q_out must be [{rows}, {d.num_q_heads}, {d.head_dim}]")
+                q_out = torch.empty((rows, self.q_heads, HEAD_DIM), dtype=torch.bfloat16, device=q.device)
+            else:
+                _need("q_out", q_out, torch.bfloat16, dev, (rows, self.q_heads, HEAD_DIM))
+        elif q_out is not None:
+            raise ValueError("q_out needs q")
+        self._check_pages(k_pages, v_pages, block_tables, seqs)
+        _need("seq_lens", seq_lens, torch.int32, dev, (seqs,))
+        if q_starts is not None:
+            _need("q_starts", q_starts, torch.int32, dev, (seqs,))
+            _need("q_lens", q_lens, torch.int32, dev, (seqs,))
+        elif seqs != rows:
+            raise ValueError(f"without q_starts, seq_lens must be [{rows}]")
         r = None
         if rotary is not None:
-            for name, t, dt, n in (("inv_freq", rotary.inv_freq, torch.float32, None),
-                                   ("positions", rotary.positions, torch.int32, rows),
-                                   ("q_norm", rotary.q_norm, torch.bfloat16, d.head_dim),
-                                   ("k_norm", rotary.k_norm, torch.bfloat16, d.head_dim)):
-                if t is None:
-                    continue
-                _check_tensors(self.device, ((name, t, dt),))
-                if t.dim() != 1 or (n is not None and t.shape[0] != n):
-                    raise ValueError(f"{name} must be a vector" + ("" if n is None else f" of {n}"))
-            freqs = rotary.inv_freq
-            r = ctypes.byref(CtxRotary(_ptr(freqs), _ptr(rotary.positions), _ptr(rotary.q_norm), _ptr(rotary.k_norm),
-                                       float(rotary.norm_eps), 0 if freqs is None else 2 * freqs.shape[0],
+            freqs, positions, q_norm, k_norm = rotary.inv_freq, rotary.positions, rotary.q_norm, rotary.k_norm
+            if freqs is not None:
+                _need("inv_freq", freqs, torch.float32, dev, (freqs.shape[0],))
+            if positions is not None:
+                _need("positions", positions, torch.int32, dev, (rows,))
+            if q_norm is not None:
+                _need("q_norm", q_norm, torch.bfloat16, dev, (HEAD_DIM,))
+            if k_norm is not None:
+                _need("k_norm", k_norm, torch.bfloat16, dev, (HEAD_DIM,))
+            r = ctypes.byref(CtxRotary(_ptr(freqs), _ptr(positions), _ptr(q_norm), _ptr(k_norm), rotary.norm_eps,
+                                       0 if freqs is None else 2 * freqs.shape[0],
                                        CTX_ROTARY_INTERLEAVED if rotary.interleaved else 0))
-        sp = _stream_ptr(stream)
         rc = self.lib.ctx_kv_append_run_paged(
-            self.handle, _ptr(q), strides[0], k.data_ptr(), strides[1], v.data_ptr(), strides[2], k_pages.data_ptr(),
+            self.handle, _ptr(q), q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, k_pages.data_ptr(),
             v_pages.data_ptr(), k_pages.shape[0], block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(),
-            _ptr(q_starts), _ptr(q_lens), seqs, rows, r, _ptr(q_out), sp)
+            _ptr(q_starts), _ptr(q_lens), seqs, rows, r, _ptr(q_out), _stream_ptr(stream))
         if rc != CTX_OK:
             raise error_for(self.lib, rc)
         return q_out
@@ -448,23 +458,17 @@ class DecodeAttention:
 
         if self.handle is None:
             raise RuntimeError("handle is closed")
-        d = self.desc
-        b = seq_lens.shape[0]
-        _check_tensors(self.device, (("q", q, torch.bfloat16), ("seq_lens", seq_lens, torch.int32),
-                                     ("q_starts", q_starts, torch.int32), ("q_lens", q_lens, torch.int32),
-                                     ("out", out, self.out_dtype)))
-        if q.dim() != 3 or q.shape[1:] != (d.num_q_heads, d.head_dim) or out.shape != q.shape:
-            raise ValueError(f"q/out must be [rows, {d.num_q_heads}, {d.head_dim}]")
+        dev, b, rows = self.device, seq_lens.shape[0], q.shape[0]
+        _need("q", q, torch.bfloat16, dev, (rows, self.q_heads, HEAD_DIM))
+        _need("out", out, self.out_dtype, dev, (rows, self.q_heads, HEAD_DIM))
+        for name, t in (("seq_lens", seq_lens), ("q_starts", q_starts), ("q_lens", q_lens)):
+            _need(name, t, torch.int32, dev, (b,))
         self._check_pages(k_pages, v_pages, block_tables, b)
-        if seq_lens.shape != (b,) or q_starts.shape != (b,) or q_lens.shape != (b,):
-            raise ValueError(f"seq_lens, q_starts, q_lens must all be [{b}]")
-        sc = None
-        if scores is not None:
-            sc = ctypes.byref(_scores_struct(scores, self.device, d.num_q_heads, b, q.shape[0]))
         rc = self.lib.ctx_prefill_attn_run_paged(
             self.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), k_pages.shape[0],
             block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(), q_starts.data_ptr(),
-            q_lens.data_ptr(), b, q.shape[0], int(max_q_len), float(scale), sc, out.data_ptr(), _stream_ptr(stream))
+            q_lens.data_ptr(), b, rows, max_q_len, scale, _scores_struct(scores, dev, self.q_heads, b, rows),
+            out.data_ptr(), _stream_ptr(stream))
         if rc != CTX_OK:
             raise error_for(self.lib, rc)
         return out
