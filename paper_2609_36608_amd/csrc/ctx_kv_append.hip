@@ -78,8 +78,11 @@ __device__ __forceinline__ int row_sequence(const AppendArgs& a, int j, int lane
   return -1;
 }
 
+// How a call's rows pass the caches: as they are, written past them, or read past them too.
+enum Stream { kCached, kStreamOut, kStreamBoth };
+
 // kRowWaves waves share the heads of a row.
-template <int kRowWaves, bool kNorm, bool kInterleaved>
+template <int kRowWaves, int kStream, bool kNorm, bool kInterleaved>
 __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a) {
   __shared__ __attribute__((aligned(16))) float2 lds_turn[kWaves][kAngles];  // cosine, sine
   const int lane = threadIdx.x & 63;
@@ -167,7 +170,8 @@ __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a) {
     }
     const bool live = h < heads && (is_q || slot >= 0);
     u32x4 x = {0u, 0u, 0u, 0u};
-    if (live) x = *reinterpret_cast<const u32x4*>(src + hl * kLaneDims);
+    if (live)
+      x = kStream == kStreamBoth ? load16(src + hl * kLaneDims) : *reinterpret_cast<const u32x4*>(src + hl * kLaneDims);
     float f[kLaneDims];
     unpack8(x, f);
     if (kNorm) {
@@ -202,18 +206,27 @@ __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a) {
     for (int i = 0; i < 4; ++i)
       y[i] = hl < rot_lanes ? pack_bf16x2(o[2 * i], o[2 * i + 1]) : pack_bf16x2(f[2 * i], f[2 * i + 1]);
     if (!is_q && !is_k) y = x;
-    if (live) *reinterpret_cast<u32x4*>(dst + hl * kLaneDims) = y;
+    if (live) {
+      if constexpr (kStream != kCached)
+        __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>(dst + hl * kLaneDims));
+      else
+        *reinterpret_cast<u32x4*>(dst + hl * kLaneDims) = y;
+    }
   }
 }
 
-template <int kRowWaves, bool kNorm>
-void launch_append(const AppendArgs& a, bool interleaved, hipStream_t s) {
+template <int kRowWaves, int kStream>
+void launch_append(const AppendArgs& a, bool norm, bool interleaved, hipStream_t s) {
   constexpr int kRows = kWaves / kRowWaves;
   const dim3 grid((unsigned)((a.rows + kRows - 1) / kRows)), block(64 * kWaves);
-  if (interleaved)
-    hipLaunchKernelGGL((kv_append_kernel<kRowWaves, kNorm, true>), grid, block, 0, s, a);
+  if (norm && interleaved)
+    hipLaunchKernelGGL((kv_append_kernel<kRowWaves, kStream, true, true>), grid, block, 0, s, a);
+  else if (norm)
+    hipLaunchKernelGGL((kv_append_kernel<kRowWaves, kStream, true, false>), grid, block, 0, s, a);
+  else if (interleaved)
+    hipLaunchKernelGGL((kv_append_kernel<kRowWaves, kStream, false, true>), grid, block, 0, s, a);
   else
-    hipLaunchKernelGGL((kv_append_kernel<kRowWaves, kNorm, false>), grid, block, 0, s, a);
+    hipLaunchKernelGGL((kv_append_kernel<kRowWaves, kStream, false, false>), grid, block, 0, s, a);
 }
 
 int check_stride(const char* name, int64_t stride, int64_t heads) {
@@ -299,11 +312,17 @@ extern "C" int ctx_kv_append_run_paged(ctx_decode_attn* h, const void* q, int64_
   const bool interleaved = (r.flags & CTX_ROTARY_INTERLEAVED) != 0;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   // A row per wave once that fills the chip (16 waves per CU); before, its heads are
-  // shared by the 4 waves of a workgroup.
-  if ((int64_t)a.rows >= 16 * (int64_t)h->num_cus)
-    norm ? launch_append<1, true>(a, interleaved, s) : launch_append<1, false>(a, interleaved, s);
+  // shared by the 4 waves of a workgroup.  Calls of that size write past the caches, and
+  // those that move more than the 256 MiB last-level cache read past them too: 28,000 rows
+  // of 32/8 heads 156 us, 146 and 142.  (Smaller calls find in it what the projection
+  // has just written: 9,600 rows and their prefill 192 us, 206 with both.)
+  const int64_t moved = (int64_t)a.rows * (a.hq + 2 * a.hkv) * kHeadDim * 2 * 2;
+  if ((int64_t)a.rows < 16 * (int64_t)h->num_cus)
+    launch_append<kWaves, kCached>(a, norm, interleaved, s);
+  else if (moved <= (int64_t)256 << 20)
+    launch_append<1, kStreamOut>(a, norm, interleaved, s);
   else
-    norm ? launch_append<kWaves, true>(a, interleaved, s) : launch_append<kWaves, false>(a, interleaved, s);
+    launch_append<1, kStreamBoth>(a, norm, interleaved, s);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(e, "kernel launch");
   return CTX_OK;
