@@ -105,7 +105,7 @@ int ctx_kv_append_run_paged(ctx_decode_attn* handle, const void* q, int64_t q_st
  * times their values; a query that sees none gets zeros.
  */
 typedef struct {
-  float softcap;              /* > 0, or 0: no cap */
+  float softcap;              /* > 0 (up to 1e38, and scale / softcap too), or 0: no cap */
   int32_t window;             /* > 0, or 0: no window */
   const float* slopes;        /* float [Hq], finite, or NULL: no bias */
   const int32_t* prefix_lens; /* int32 [num_seqs] or NULL: no prefix; a value past L_b counts as L_b */

@@ -175,12 +175,19 @@ constexpr int32_t kMostTokens = 1 << 30;  // in paged caches: rows and positions
     return fail(CTX_ERR_INVALID_ARG, "num_pages must not be negative and max_pages_per_seq must be positive");
   if ((int64_t)num_pages * h->desc.page_tokens > kMostTokens)
     return fail(CTX_ERR_UNSUPPORTED, "caches of more than %d tokens", kMostTokens);
-  if (!(std::isfinite(sc.softcap) && sc.softcap >= 0.f))
-    return fail(CTX_ERR_INVALID_ARG, "softcap must be finite and >= 0");
-  if (sc.softcap > 0.f && !std::isfinite(scale / sc.softcap))
-    return fail(CTX_ERR_INVALID_ARG, "scale / softcap is not finite");
+  // both in log2 units and twice that stay finite
+  if (!(sc.softcap >= 0.f && sc.softcap <= 1e38f))
+    return fail(CTX_ERR_INVALID_ARG, "softcap must be in [0, 1e38]");
+  if (sc.softcap > 0.f && !(std::fabs(scale / sc.softcap) <= 1e38f))
+    return fail(CTX_ERR_INVALID_ARG, "scale / softcap must be in [-1e38, 1e38]");
   if (sc.window < 0) return fail(CTX_ERR_INVALID_ARG, "window %d < 0", sc.window);
   return CTX_OK;
+}
+
+// The cap of a call, 0 where it is so far above any score that scale / softcap has no
+// normal float: tanh(y) is y there.
+[[maybe_unused]] float cap_of(const ctx_attn_scores& sc, float scale) {
+  return sc.softcap > 0.f && std::fabs(scale / sc.softcap) >= 1.17549435e-38f ? sc.softcap : 0.f;
 }
 
 int check_device(ctx_decode_attn* h) {

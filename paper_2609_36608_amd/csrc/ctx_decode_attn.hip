@@ -172,11 +172,11 @@ struct SeenSpans {
   int32_t most;                // tokens that a row of the block table can name
   __device__ __forceinline__ Seen seen(int b) const {
     Seen s;
-    const int len = lens[b];
+    const int len = lens[b];  // the newest token is at len - 1 also where the table ends before it
     s.len = len < 0 ? 0 : len < most ? len : most;
     const int prefix = prefix_lens != nullptr ? prefix_lens[b] : 0;
     s.prefix = prefix < 0 ? 0 : prefix < s.len ? prefix : s.len;
-    s.low = window > 0 && window < s.len ? s.len - window : 0;
+    s.low = window > 0 && window < len ? len - window : 0;
     if (doc_starts != nullptr) {
       const int doc = doc_starts[b];
       s.low = doc > s.low ? doc : s.low;
@@ -1158,8 +1158,8 @@ extern "C" int ctx_decode_attn_run_paged_scored(ctx_decode_attn* h, const void* 
   const int64_t most = (int64_t)max_pages_per_seq * h->desc.page_tokens;
   const SeenSpans spans{seq_lens, sc.prefix_lens, sc.doc_starts, sc.window,
                         (int32_t)(most < kMostTokens ? most : kMostTokens)};
-  const Scores sco{sc.softcap > 0.f ? scale / sc.softcap : 0.f, (float)((double)sc.softcap * 1.4426950408889634),
-                   sc.slopes};
+  const float cap = cap_of(sc, scale);
+  const Scores sco{cap > 0.f ? scale / cap : 0.f, (float)((double)cap * 1.4426950408889634), sc.slopes};
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (h->desc.out_dtype == CTX_DTYPE_F32)
     launch_scored<float>(h, p, sco, spans, q, k_pages, v_pages, block_tables, max_pages_per_seq, num_pages, out, s);

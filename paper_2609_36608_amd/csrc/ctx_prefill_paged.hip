@@ -60,7 +60,12 @@ constexpr int kNowhere = 0x7ffffff0;  // a byte offset past every range
 constexpr int kHeld = 64;   // half blocks whose cache rows a wave holds
 
 // what a kernel changes of the scores
-enum Change { kPlain, kBias, kCap, kCapBias };
+enum Change { kPlain, kBias, kCap, kCapBias, kFar, kFarBias };  // kFar: a cap far above the scores
+
+// Caps from which a score of its own precision counts among bf16 weights too: up to here
+// 2^-23 of the cap, in log2 units, is within 1e-4.  Such a cap hardly changes anything, so
+// these calls have one kernel, of one tile per wave.
+constexpr float kFarFrom = 512.f;
 
 // s_waitcnt vmcnt(n) with expcnt and lgkmcnt left open
 constexpr int wait_vmcnt(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }
@@ -151,8 +156,9 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
     OutT* __restrict__ out) {
   constexpr bool kSplitKv = kSplit > 0;
   constexpr int kWaves = wg_waves(kSplit);
-  constexpr bool kHasBias = kChange == kBias || kChange == kCapBias;
-  constexpr bool kHasCap = kChange == kCap || kChange == kCapBias;
+  constexpr bool kHasBias = (kChange & 1) != 0;
+  constexpr bool kHasCap = kChange >= kCap;
+  constexpr bool kFarCap = kChange >= kFar;
   constexpr int kTerms = sizeof(OutT) == 4 ? 3 : 1;
   constexpr int kCols = (kSplitKv ? 1 : kWaves) * kTiles * 16;
   constexpr int kStagers = kSplitKv ? 1 : kWaves;  // waves that stage a block together
@@ -199,7 +205,8 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
   const int seq_len = pp.lens[b] < 0 ? 0 : pp.lens[b];
   const int hist = seq_len - new_tokens;  // position of query 0
   const int64_t named = (int64_t)pp.max_pages * pp.page_tokens;
-  const int tokens = seq_len < named ? seq_len : (int)named;  // that the table can name
+  int tokens = seq_len < named ? seq_len : (int)named;  // that the table can name
+  tokens = tokens < kMostTokens ? tokens : kMostTokens;
   int prefix = pp.prefix_lens != nullptr ? pp.prefix_lens[b] : 0;
   prefix = prefix < 0 ? 0 : prefix < tokens ? prefix : tokens;
   const size_t row_elems = (size_t)pp.hkv * kHeadDim;
@@ -458,7 +465,7 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
     };
     if constexpr (!kHasCap) {
       each(0.f, [&](float x, float add) __attribute__((always_inline)) { return fmaf(x, pp.factor, add); });
-    } else if constexpr (kTerms == 1) {
+    } else if constexpr (kTerms == 1 && !kFarCap) {
       // tanh(y) = 1 - 2 / (e^2y + 1), 2^-23 of the cap off: far below a bf16 weight's
       // rounding.  (An odd polynomial up to |y| = 1, 7 instructions for 5, and a test
       // whether a block's scores all lie there took as long: 100 requests over long
@@ -830,8 +837,10 @@ void launch_paged(const PagedArgs& a, int change, int split, int tiles) {
     launch_change<OutT, kBias>(a, split, tiles);
   else if (change == kCap)
     launch_change<OutT, kCap>(a, split, tiles);
-  else
+  else if (change == kCapBias)
     launch_change<OutT, kCapBias>(a, split, tiles);
+  else if constexpr (sizeof(OutT) == 2)
+    change == kFar ? launch_split<OutT, kFar, 0, 1>(a) : launch_split<OutT, kFarBias, 0, 1>(a);
   if (a.plan.splits > 1) {
     const int64_t parts = (int64_t)a.plan.total_q * a.plan.hq;
     hipLaunchKernelGGL((prefill_join_kernel<OutT>), dim3((unsigned)((parts + kJoinWaves - 1) / kJoinWaves)),
@@ -852,6 +861,7 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   if (scores != nullptr) sc = *scores;
   rc = check_scored(h, sc, scale, num_pages, max_pages_per_seq);
   if (rc != CTX_OK) return rc;
+  sc.softcap = cap_of(sc, scale);
   if (total_q < 0 || max_q_len < 0)
     return fail(CTX_ERR_INVALID_ARG, "total_q and max_q_len must not be negative (%d, %d)", total_q, max_q_len);
   if (num_seqs == 0 || max_q_len == 0 || total_q == 0) return CTX_OK;
@@ -901,7 +911,8 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   // waves 42, wide 82).  Not for short contexts, which leave a wave few blocks: 400 fresh
   // tokens 13.5 us wide, 15.8 narrow.
   const int64_t narrow = grid_of(most_tiles * 16);
-  const int split = context <= 16 * kBlock || narrow > 2 * cus ? 0 : narrow > cus ? 4 : 8;
+  const bool far_cap = d.out_dtype != CTX_DTYPE_F32 && sc.softcap > kFarFrom;
+  const int split = far_cap || context <= 16 * kBlock || narrow > 2 * cus ? 0 : narrow > cus ? 4 : 8;
   // Wide ones have fewer tiles per wave where there would be too few to fill the chip: one
   // tile as long as all workgroups are resident (three per CU), two (of three) as long as
   // about all are (two per CU).  Of 1, 2 and 3 tiles: 1,024 new tokens over 4,000 117, 124
@@ -909,7 +920,7 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   // 600 24, 26 and 32, with up to 300 54, 59 and 46.
   const auto wide = [&](int t) { return grid_of(kWideWaves * t * 16); };
   const int tiles = split > 0             ? most_tiles
-                    : wide(1) <= 3 * cus ? 1
+                    : far_cap || wide(1) <= 3 * cus ? 1
                     : most_tiles > 2 && 4 * wide(2) <= 9 * cus ? 2
                                                                : most_tiles;
   // Where 8-wave workgroups are fewer than the CUs several share a tile's blocks, through
@@ -934,7 +945,7 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   const PagedArgs a{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k_pages),
                     static_cast<const uint16_t*>(v_pages), pp, out, (unsigned)blocks,
                     reinterpret_cast<hipStream_t>(stream)};
-  const int change = (sc.softcap > 0.f ? kCap : kPlain) + (sc.slopes != nullptr ? kBias : kPlain);
+  const int change = (far_cap ? kFar : sc.softcap > 0.f ? kCap : kPlain) + (sc.slopes != nullptr ? kBias : kPlain);
   if (d.out_dtype == CTX_DTYPE_F32)
     launch_paged<float>(a, change, split, tiles);
   else

@@ -227,6 +227,7 @@ def test_pages_outside_the_cache_are_not_seen(wide):
     check(bt, torch.bfloat16, window=60, prefix=[20, 0, 17], **kw)
     bt.table = np.ascontiguousarray(bt.table[:, :3])  # and tokens past the table
     check(bt, slopes=slopes_of(16), **kw)
+    check(bt, torch.bfloat16, window=100, prefix=[20, 0, 17], **kw)
 
 
 @pytest.mark.parametrize("hist", [1000, 1024, 2100])
@@ -272,6 +273,15 @@ def test_large_logits_and_a_zero_scale():
     bt.k[~bt.k.isnan()] *= 2.0 ** 60  # every score at its cap
     check(bt, torch.bfloat16, softcap=1.0)
     check(bt, softcap=1.0)
+
+
+@pytest.mark.parametrize("softcap", [1e-3, 500.0, 600.0, 1e5, 1e38])
+def test_caps_from_tiny_to_far_above_the_scores(softcap):
+    bt = Batch(61, [300, 90], [120, 2], 16, 16, 8)
+    bt.q[::3] *= 8
+    for kw in (dict(), dict(slopes=slopes_of(16), window=70)):
+        check(bt, torch.bfloat16, softcap=softcap, share=8.0, **kw)
+        check(bt, softcap=softcap, share=8.0, **kw)
 
 
 def test_rising_and_falling_scores():
@@ -334,6 +344,9 @@ def test_refusals():
 
         call()
         for kw, status in ((dict(scores=AttnScores(softcap=-1.0)), bd.CTX_ERR_INVALID_ARG),
+                           (dict(scores=AttnScores(softcap=2e38)), bd.CTX_ERR_INVALID_ARG),
+                           (dict(scores=AttnScores(softcap=1e-40)), bd.CTX_ERR_INVALID_ARG),
+                           (dict(scores=AttnScores(softcap=float("nan"))), bd.CTX_ERR_INVALID_ARG),
                            (dict(scores=AttnScores(window=-1)), bd.CTX_ERR_INVALID_ARG),
                            (dict(scale=float("nan")), bd.CTX_ERR_INVALID_ARG),
                            (dict(max_q_len=-1), bd.CTX_ERR_INVALID_ARG)):

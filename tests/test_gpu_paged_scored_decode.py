@@ -149,6 +149,8 @@ def test_pages_outside_the_cache_are_not_seen():
     bt.table = np.ascontiguousarray(bt.table[:, :2])  # tokens past the table
     bt.table[2, 0] = bt.table[2, 1]
     check(bt)
+    check(bt, window=80, slopes=slopes_of(16))  # the window counts from the newest token
+    check(bt, window=30, prefix=[5, 0, 17, 33])
 
 
 def test_large_logits_and_a_zero_scale():
