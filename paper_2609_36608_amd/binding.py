@@ -342,7 +342,7 @@ class DecodeAttention:
             rc = self.lib.ctx_decode_attn_run_paged_scored(
                 self.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), k_pages.shape[0],
                 block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(), b, scale,
-                _scores_struct(scores, dev, self.q_heads, b, b), out.data_ptr(), _stream_ptr(stream))
+                _scores_struct(scores, dev, self.q_heads, b, b), out.data_ptr(), self._stream(stream))
             if rc != CTX_OK:
                 raise error_for(self.lib, rc)
             return out
@@ -380,6 +380,12 @@ class DecodeAttention:
         _need("k_pages", k_pages, torch.bfloat16, self.device, pages)
         _need("v_pages", v_pages, torch.bfloat16, self.device, pages)
         _need("block_tables", block_tables, torch.int32, self.device, (seqs, block_tables.shape[-1]))
+
+    def _stream(self, stream):
+        import torch
+
+        # of the handle's device, which the call checks to be the current one
+        return torch._C._cuda_getCurrentRawStream(self.device) if stream is None else _stream_ptr(stream)
 
     def _row_stride(self, name: str, t, rows: int, heads: int) -> int:
         """Elements between the rows of heads that may be slices of wider rows."""
@@ -444,7 +450,7 @@ class DecodeAttention:
         rc = self.lib.ctx_kv_append_run_paged(
             self.handle, _ptr(q), q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, k_pages.data_ptr(),
             v_pages.data_ptr(), k_pages.shape[0], block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(),
-            _ptr(q_starts), _ptr(q_lens), seqs, rows, r, _ptr(q_out), _stream_ptr(stream))
+            _ptr(q_starts), _ptr(q_lens), seqs, rows, r, _ptr(q_out), self._stream(stream))
         if rc != CTX_OK:
             raise error_for(self.lib, rc)
         return q_out
@@ -468,7 +474,7 @@ class DecodeAttention:
             self.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), k_pages.shape[0],
             block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(), q_starts.data_ptr(),
             q_lens.data_ptr(), b, rows, max_q_len, scale, _scores_struct(scores, dev, self.q_heads, b, rows),
-            out.data_ptr(), _stream_ptr(stream))
+            out.data_ptr(), self._stream(stream))
         if rc != CTX_OK:
             raise error_for(self.lib, rc)
         return out
