@@ -55,7 +55,9 @@ extern "C" {
  *                CTX_ROTARY_INTERLEAVED.  The other dimensions stay.
  *
  * The result is computed in fp32 from the bf16 inputs and rounded to bf16 once;
- * the angle is reduced in fp64, so far positions are as exact as near ones.
+ * the angle is reduced in fp64, so far positions are as exact as near ones.  The sum of
+ * squares is an fp32 one: a normed head holds values up to 1e18, and with norm_eps = 0
+ * some of 1e-18 or more.
  */
 #define CTX_ROTARY_INTERLEAVED 1u
 typedef struct {
@@ -107,7 +109,7 @@ int ctx_kv_append_run_paged(ctx_decode_attn* handle, const void* q, int64_t q_st
 typedef struct {
   float softcap;              /* > 0 (up to 1e38, and scale / softcap too), or 0: no cap */
   int32_t window;             /* > 0, or 0: no window */
-  const float* slopes;        /* float [Hq], finite, or NULL: no bias */
+  const float* slopes;        /* float [Hq], |slope| * L_b up to 1e37, or NULL: no bias */
   const int32_t* prefix_lens; /* int32 [num_seqs] or NULL: no prefix; a value past L_b counts as L_b */
   const int32_t* doc_starts;  /* int32, the first token of each query's document, one per packed
                                  row (prefill) or sequence (decode), or NULL: 0.  A value above p

@@ -232,6 +232,7 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
   bf16x8 qb[kTiles][4];
   // over the wave's rows: what some row sees past the prefix, what all see
   int some_low = INT_MAX, some_last = -1, all_low = 0, all_last = INT_MAX;
+  int gap = INT_MAX;  // first position that its own row does not see
 #pragma unroll
   for (int ct = 0; ct < kTiles; ++ct) {
     const int col = (col_wave * kTiles + ct) * 16 + n;
@@ -240,11 +241,12 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
     const int qi = (tile * kCols + col) / g;
     const int head = kv * g + (tile * kCols + col - qi * g);
     const int64_t row = (int64_t)row0 + qi;
+    const int p = hist + qi;
     low[ct] = 0;
     last[ct] = 0;
     slope[ct] = 0.f;
+    bool sees_own = qi >= nq;  // or is no row
     if (valid) {
-      const int p = hist + qi;
       const int doc = pp.doc_starts != nullptr ? pp.doc_starts[row] : 0;
       int lo = pp.window > 0 && p >= pp.window ? p - pp.window + 1 : 0;
       lo = doc > lo ? doc : lo;
@@ -255,6 +257,7 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
         last[ct] = p;
         some_low = lo < some_low ? lo : some_low;
         some_last = end > some_last ? end : some_last;
+        sees_own = true;
       } else {
         low[ct] = INT_MAX;
         last[ct] = p < prefix ? p : prefix - 1;
@@ -268,16 +271,19 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) qb[ct][kk] = as_bf16x8(u32x4{0u, 0u, 0u, 0u});
     }
+    gap = !sees_own && p < gap ? p : gap;
   }
   some_low = columns_extreme<true>(some_low);
   some_last = columns_extreme<false>(some_last);
   all_low = columns_extreme<false>(all_low);
   all_last = columns_extreme<true>(all_last);
+  gap = columns_extreme<true>(gap);
   // the same over the workgroup: the tokens it reads
   int first = some_low, until = some_last + 1;
   if constexpr (!kSplitKv) {
-    __shared__ int lds_seen[2][kWaves];
+    __shared__ int lds_seen[3][kWaves];
     if (lane == 0) {
+      lds_seen[2][wave] = gap;
       lds_seen[0][wave] = some_low;
       lds_seen[1][wave] = some_last + 1;
     }
@@ -286,11 +292,31 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
     for (int w = 0; w < kWaves; ++w) {
       first = lds_seen[0][w] < first ? lds_seen[0][w] : first;
       until = lds_seen[1][w] > until ? lds_seen[1][w] : until;
+      gap = lds_seen[2][w] < gap ? lds_seen[2][w] : gap;
     }
+    gap = __builtin_amdgcn_readfirstlane(gap);
     first = __builtin_amdgcn_readfirstlane(first);
     until = __builtin_amdgcn_readfirstlane(until);
   }
   const int end = until > prefix ? until : prefix;  // tokens from here on are not seen
+  // From gap on there may be tokens between first and until that no row sees: a padding
+  // row's position, unless a later row's document takes it in.
+  const int own = hist + first_q;  // position of the workgroup's first row
+  __shared__ uint8_t lds_hidden[kCols];  // of own, own + 1, ...
+  if (gap < until) {
+    const int rows = ((tile + 1) * kCols + g - 1) / g < nq ? ((tile + 1) * kCols + g - 1) / g - first_q : nq - first_q;
+    for (int i = tid; i < rows; i += 64 * kWaves) {
+      bool seen = false;
+      for (int r = i; r < rows && !seen; ++r) {
+        const int64_t row = (int64_t)row0 + first_q + r;
+        if (row < 0 || row >= pp.total_q) continue;
+        const int doc = pp.doc_starts != nullptr ? pp.doc_starts[row] : 0;
+        seen = doc <= own + i && (pp.window == 0 || r - i < pp.window);
+      }
+      lds_hidden[i] = !seen;
+    }
+    __syncthreads();
+  }
   const int hole = (prefix + kBlock - 1) & -kBlock;
   const int skip = first < until && (first & -kBlock) > hole ? (first & -kBlock) - hole : 0;
   const int v_end = end - skip;
@@ -327,9 +353,8 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
   }
 
   // Of the halves of the wave's next kHeld / 2 blocks, from `held` of the order on, one per
-  // lane: its first cache
-  // row / 16, whether it has tokens between prefix and `first` (kEdge), and its tokens
-  // that are seen at all; 0 outside the cache and past the end.
+  // lane: its first cache row / 16, whether it may have tokens past the prefix that no row
+  // sees (kEdge), and its tokens before the end; 0 outside the cache and past the end.
   constexpr uint32_t kEdge = 32;
   constexpr int kStep = kSplitKv ? kWaves * kBlock : kBlock;  // between a wave's blocks
   int held = 0;
@@ -346,7 +371,7 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
         const int page = pp.block_tables[(size_t)b * pp.max_pages + j];
         if (page >= 0 && page < pp.num_pages) {
           const int row = page * pp.page_tokens + (t - j * pp.page_tokens);
-          const uint32_t edge = t < first && t + kHalf > prefix ? kEdge : 0u;
+          const uint32_t edge = ((t < first) | ((t + kHalf > gap) & (t < until))) && t + kHalf > prefix ? kEdge : 0u;
           halves = (uint32_t)(row / kHalf) << 6 | edge | (uint32_t)(end - t < kHalf ? end - t : kHalf);
         }
       }
@@ -373,7 +398,7 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
   auto absent_of = [](const Words& w) { return ((w.h[0] & 31) == 0 ? 1 : 0) | ((w.h[1] & 31) == 0 ? 2 : 0); };
   // A block's loads, one instruction stream for every block (with a stream of its own for
   // ordinary blocks the compiler lost count of the loads in flight and waited for all):
-  // outside the cache, past the end and, of values, between prefix and `first` zeros are
+  // outside the cache, past the end and, of values, where no row sees the token zeros are
   // written.  (Whatever keys give there is masked.)
   auto load_block = [&](const uint16_t* base, bool values, const Words& w, int u, uint16_t* dst)
       __attribute__((always_inline)) {
@@ -388,7 +413,9 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
           const int x = t + h * kHalf + (r * kStagers + stage_wave) * 4 + (lane >> 4);
-          off[h][r] = (x >= prefix) & (x < first) ? kNowhere : offset[r];
+          bool hidden = x < first;
+          if (x >= gap && x < until) hidden = lds_hidden[x - own] != 0;
+          off[h][r] = x >= prefix && hidden ? kNowhere : offset[r];
         }
     }
 #pragma unroll
@@ -938,7 +965,7 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   pp.o_ws = h->o_ws;
   pp.ml_ws = h->ml_ws;
   const int64_t blocks = split > 0 ? narrow * pp.splits : wide(tiles);
-  if (units > INT32_MAX || blocks > INT32_MAX) return fail(CTX_ERR_INVALID_ARG, "prefill grid too large");
+  if (units > INT32_MAX || blocks > INT32_MAX || cols > kMostTokens) return fail(CTX_ERR_INVALID_ARG, "prefill grid too large");
   pp.units = (int32_t)units;
   pp.tiles = (int32_t)(blocks / pp.splits / units);
   pp.last_first = split == 0 && blocks > 2 * cus;

@@ -211,6 +211,39 @@ def test_unseen_slots_may_hold_anything(wide):
     assert torch.equal(got, clean) and got[live].isfinite().all()
 
 
+@pytest.mark.parametrize("kind", ["wide1", "wide2", "wide3", "narrow4", "narrow8"])
+@pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
+def test_padding_rows_between_documents_may_hold_anything(kind, out_dtype):
+    """NaN and infinities at the positions of padding rows that no later row's document takes in,
+    beside padding rows that a later row sees."""
+    bt, bound = kind_batch(kind)
+    rng = np.random.default_rng(9)
+    docs = np.zeros(bt.rows, np.int64)
+    prefix = rng.integers(0, 40, len(bt.lens))
+    hidden = 0
+    for b, (n, m) in enumerate(zip(bt.lens, bt.new)):
+        seen = torch.arange(max(n, 0)) < int(prefix[b])
+        first, i = 0, 0
+        while i < m:
+            for _ in range(min(int(rng.integers(1, 25)), m - i)):  # a document
+                docs[bt.starts[b] + i] = first
+                seen[first:n - m + i + 1] = True
+                i += 1
+            pads = min(int(rng.integers(0, 9)), m - i)
+            docs[bt.starts[b] + i:bt.starts[b] + i + pads] = 2 ** 31 - 1
+            i += pads
+            first = n - m + i - int(rng.integers(0, 4) if rng.random() < 0.3 else 0)
+        for t in torch.nonzero(~seen)[:, 0].tolist():
+            bt.k[bt.slot(b, t)] = float("nan")
+            bt.v[bt.slot(b, t)] = float("inf") if t % 2 else float("nan")
+            hidden += 1
+    assert hidden > 10
+    got, live = run(bt, out_dtype=out_dtype, docs=docs, prefix=prefix, max_seq_len=bound)
+    bt.k, bt.v = bt.k.nan_to_num(0.0, 0.0), bt.v.nan_to_num(0.0, 0.0)
+    ref, spread = attention_reference(bt, SCALE, docs=docs, prefix=prefix, spread=True)
+    close(got, live, ref, spread, out_dtype)
+
+
 @pytest.mark.parametrize("wide", [False, True])
 def test_pages_outside_the_cache_are_not_seen(wide):
     lens, new = ([700, 100, 90], [600, 50, 90]) if wide else ([200, 100, 90], [70, 50, 90])
