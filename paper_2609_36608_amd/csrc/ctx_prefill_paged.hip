@@ -301,9 +301,10 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
   const int end = until > prefix ? until : prefix;  // tokens from here on are not seen
   // From gap on there may be tokens between first and until that no row sees: a padding
   // row's position, unless a later row's document takes it in.
-  const int own = hist + first_q;  // position of the workgroup's first row
-  __shared__ uint8_t lds_hidden[kCols];  // of own, own + 1, ...
-  if (gap < until) {
+  const bool gaps = gap < until && prefix < until;
+  const int own = gaps ? hist + first_q : INT_MAX;  // position of the workgroup's first row
+  __shared__ uint8_t lds_hidden[kCols + kBlock];    // whether own, own + 1, ... are such tokens
+  if (gaps) {
     const int rows = ((tile + 1) * kCols + g - 1) / g < nq ? ((tile + 1) * kCols + g - 1) / g - first_q : nq - first_q;
     for (int i = tid; i < rows; i += 64 * kWaves) {
       bool seen = false;
@@ -362,8 +363,10 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
   auto look_up = [&](int u) __attribute__((always_inline)) {
     held = u;
     halves = 0;
-    const int mine = u + (lane >> 1) * kStep;
-    const int at = block_at(mine) + (lane & 1) * kHalf;
+    int half = lane;
+    asm volatile("" : "+v"(half));  // nothing of this is kept in a register for the next time
+    const int mine = u + (half >> 1) * kStep;
+    const int at = block_at(mine) + (half & 1) * kHalf;
     const int t = token(at);
     if (mine < share_end && at < v_end) {
       const int j = t / pp.page_tokens;
@@ -371,7 +374,7 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
         const int page = pp.block_tables[(size_t)b * pp.max_pages + j];
         if (page >= 0 && page < pp.num_pages) {
           const int row = page * pp.page_tokens + (t - j * pp.page_tokens);
-          const uint32_t edge = ((t < first) | ((t + kHalf > gap) & (t < until))) && t + kHalf > prefix ? kEdge : 0u;
+          const uint32_t edge = ((t < first) | (t + kHalf > own)) && t + kHalf > prefix ? kEdge : 0u;
           halves = (uint32_t)(row / kHalf) << 6 | edge | (uint32_t)(end - t < kHalf ? end - t : kHalf);
         }
       }
@@ -406,16 +409,16 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
 #pragma unroll
     for (int r = 0; r < kRounds; ++r) off[0][r] = off[1][r] = offset[r];
     if (values && ((w.h[0] | w.h[1]) & kEdge)) {
-      asm volatile("");  // a branch: not worked out for every block
+      int at = lane >> 4;
+      asm volatile("" : "+v"(at));  // a branch: nothing of it worked out for every block
       const int t = token(block_at(u));
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int r = 0; r < kRounds; ++r) {
-          const int x = t + h * kHalf + (r * kStagers + stage_wave) * 4 + (lane >> 4);
-          bool hidden = x < first;
-          if (x >= gap && x < until) hidden = lds_hidden[x - own] != 0;
-          off[h][r] = x >= prefix && hidden ? kNowhere : offset[r];
+          const int x = t + h * kHalf + (r * kStagers + stage_wave) * 4 + at;
+          // x < until + kBlock, which own has kCols tokens before at most
+          if (x >= prefix && (x >= own ? lds_hidden[x - own] != 0 : x < first)) off[h][r] = kNowhere;
         }
     }
 #pragma unroll
