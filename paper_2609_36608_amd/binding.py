@@ -408,7 +408,8 @@ class DecodeAttention:
         slots of each sequence's last q_lens[b] of seq_lens[b] tokens (rows q_starts[b] ..; without
         q_starts / q_lens row b is the newest token of sequence b), and q [rows, Hq, D], if given, to
         q_out; q and k are normed and rotated as `rotary` says.  k, v and q may be slices of wider
-        rows (heads and dimensions contiguous).  Returns q_out (allocated if None, without q None)."""
+        rows (heads and dimensions contiguous).  Returns q_out (if None, allocated on the current
+        stream; without q None)."""
         import torch
 
         if self.handle is None:

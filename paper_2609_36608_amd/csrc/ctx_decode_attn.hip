@@ -34,6 +34,9 @@
 //     block's maximum exceeds it by more than 2^8, so probabilities stay
 //     <= 256 and the rescale of the accumulators is rare; the merge uses the
 //     same stale maxima, so the result is unchanged.
+//   * Changed scores (a cap, a bias by distance, a window, a prefix, documents) have a
+//     kernel of their own over paged caches, on the same ranges, tiles and products:
+//     decode_scored_kernel.  The ranges cover the blocks with seen tokens alone.
 //   * Merge: out = sum_s o_s 2^(m_s - M) / sum_s l_s 2^(m_s - M), M = max_s m_s,
 //     in fixed segment order (deterministic; no atomics).
 
@@ -72,9 +75,9 @@ constexpr int merge_waves(int seg_waves) { return seg_waves < 4 ? 4 : seg_waves;
 constexpr int kWgWaves = 8;  // most waves (KV heads of one range) per split workgroup
 constexpr int kTileBytes = 2 * kBlock * kHeadDim * 2;  // one wave's K and V tiles in LDS
 // Waves per SIMD the split kernel is compiled for: 3 for contiguous caches (159
-// VGPRs), 2 for paged ones (168, which a third wave would just fit: it is the slower
-// choice, see resident_waves).  An 8-wave workgroup (Hkv = 8) is one workgroup per
-// CU either way.
+// VGPRs), 2 for paged ones (171, 172 with changed scores; a third wave, when it fit into
+// 168, was the slower choice, see resident_waves).  An 8-wave workgroup (Hkv = 8) is one
+// workgroup per CU either way.
 constexpr int kWavesPerEu = 3;
 constexpr int kPagedWavesPerEu = 2;
 
@@ -283,9 +286,8 @@ __device__ __forceinline__ u32x4 buf_load16(__amdgpu_buffer_rsrc_t r, int voff, 
 }
 
 // Process one 16-token block.  logits(x) turns the products q.k in x (lane (c, n): tokens
-// 4c + i, query n) into logits in log2 units, -inf where a token is not seen; lds_v points at this lane's transpose-read address in the block's V tile
-// (token 4c + n / 4, dimensions 4 (n % 4) .. 4 (n % 4) + 3 of dimension group 0),
-// v_step(nb) the element offset of dimension group nb from it.
+// 4c + i, query n) into logits in log2 units, -inf where a token is not seen.  lds_v is
+// the block's V tile, v_off[nb] this lane's transpose read of dimension group nb in it.
 // kTerms: bf16 terms of each softmax weight, 2 (16 significant bits) or 3 (24).
 template <int kTerms, typename Logits>
 __device__ __forceinline__ void attend_block(const u32x4 (&kr)[4], const uint16_t* lds_v, const int (&v_off)[8],
@@ -1058,8 +1060,8 @@ template <typename OutT, int kSegWaves, typename Spans>
 void launch_merge_of(const Plan& p, const Spans& spans, const ctx_decode_attn* h, OutT* out, hipStream_t s) {
   constexpr int kHeads = merge_waves(kSegWaves) / kSegWaves;
   const dim3 grid((unsigned)(((int64_t)p.num_seqs * p.hq + kHeads - 1) / kHeads));
-  hipLaunchKernelGGL((decode_merge_kernel<OutT, kSegWaves, Spans>), grid, dim3(64 * merge_waves(kSegWaves)), 0, s, spans, p,
-                     h->o_ws, h->ml_ws, out);
+  hipLaunchKernelGGL((decode_merge_kernel<OutT, kSegWaves, Spans>), grid, dim3(64 * merge_waves(kSegWaves)), 0, s,
+                     spans, p, h->o_ws, h->ml_ws, out);
 }
 
 template <typename OutT, typename Spans>

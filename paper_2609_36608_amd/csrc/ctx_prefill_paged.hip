@@ -8,9 +8,11 @@
 // pairs of one KV group, and 32-token K/V blocks go straight from memory into LDS:
 //   * wide workgroups: 4 waves of kTiles 16-column tiles each share every block
 //     through a three-stage tile, loaded two blocks ahead;
-//   * narrow workgroups, for calls with too few columns to fill the chip: all 4 waves
-//     cover the same kTiles tiles, each with a quarter of the blocks, its own tiles and
-//     its own running maxima; they are merged through LDS in a fixed order.
+//   * narrow workgroups, for calls with too few columns to fill the chip: all 4 or 8
+//     waves cover the same kTiles tiles, each with its share of the blocks, its own LDS
+//     tiles and its own running maxima; they are merged through LDS in a fixed order.
+//     With few rows over a long context several workgroups share a tile's blocks in turn,
+//     and a second kernel joins their partial outputs.
 // Per 32 tokens and 16 columns a wave computes S^T = K Q^T (8 MFMA 16x16x32), the
 // scores' changes, the mask and an online softmax, and O^T += V^T P^T (8 MFMA per
 // bf16 term of P; V^T through the LDS transpose read).
@@ -35,6 +37,13 @@
 //   * bf16 outputs: weights rounded to bf16 and normalised by the sum of the rounded
 //     ones.  fp32 outputs: three bf16 terms (24 bits), in two tiles per wave, since
 //     three would not leave registers for them.
+
+// Bound by vector and matrix work together, at the clock that the power limit leaves: 100
+// requests with 128..512 new tokens over 4,096..12,288 (32/8 heads, 16-token pages) run at
+// 1,045..1,070 TFLOP/s, capped at 870, with slopes at 950, with both at 820; a single prompt
+// of 10,240 tokens at 1,120 with shuffled pages and at 1,212 with pages in order.  A wave
+// holds 16 columns in each of up to 3 tiles, since every K and V fragment read from LDS is
+// then used three times; a fourth would leave no registers (256 at two waves per SIMD).
 
 #include <hip/hip_runtime.h>
 
@@ -955,7 +964,9 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
                                                                : most_tiles;
   // Where 8-wave workgroups are fewer than the CUs several share a tile's blocks, through
   // the workspace and a second launch: as many as fit there, leave each a context of 512
-  // tokens and the join a wave's lanes.  16 new tokens over 20,000 30 us (142 alone).
+  // tokens and the join a wave's lanes.  16 new tokens over 20,000 29 us (142 alone).  With
+  // 256, 512 and 1,024 tokens: 16 over 2,000 15.8, 17.7 and 19.9 us, over 4,000 20.6, 18.9 and
+  // 20.8, over 8,000 22.7, 22.5 and 21.7; 5 over 3,000 14.9, 15.1 and 19.1.
   pp.splits = 1;
   if (split == 8) {
     const int64_t slots = h->max_ranges + d.max_batch;
