@@ -79,17 +79,36 @@ constexpr float kFarFrom = 512.f;
 // s_waitcnt vmcnt(n) with expcnt and lgkmcnt left open
 constexpr int wait_vmcnt(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }
 
+// Quotients of 0 <= x < 2^31 by d > 0, exact: with 2^(shift - 1) < d <= 2^shift the factor's
+// excess over 2^(31 + shift) / d is less than 1, which x / 2^31 of cannot carry the
+// quotient over the next whole number.  (Three instructions where a division takes 30, and
+// a workgroup has a dozen before its first block.)
+struct Divisor {
+  int32_t d;
+  uint32_t factor;
+  int32_t shift;
+  Divisor() = default;
+  explicit Divisor(int32_t by) : d(by), shift(0) {
+    while (((int64_t)1 << shift) < by) ++shift;
+    factor = (uint32_t)((((uint64_t)1 << (31 + shift)) + by - 1) / by);
+  }
+  __device__ __forceinline__ int of(int x) const { return (int)(__umulhi((uint32_t)x << 1, factor) >> shift); }
+};
+
 struct PagedPlan {
   const int32_t *block_tables, *lens, *q_starts, *q_lens;
   const int32_t *prefix_lens, *doc_starts;  // or null
   const float* slopes;
   int32_t window;  // or 0
-  int32_t max_pages, num_pages, page_tokens;
+  int32_t max_pages, num_pages;
+  Divisor page_tokens;
   int32_t total_q, max_q_len;
-  int32_t hq, hkv, group;
-  int32_t tiles;       // workgroups per (sequence, KV head)
+  int32_t hq;
+  Divisor hkv, group;
+  Divisor tiles;       // workgroups per (sequence, KV head)
   int32_t num_seqs;
   int32_t units;       // sequences x KV heads
+  Divisor rest;        // of them over whole XCDs, or 1
   int32_t last_first;  // the most work first
   int32_t splits;      // workgroups that share the blocks of a tile; with more than one their
   float* o_ws;         // partial outputs [splits, total_q, hq, D] and
@@ -135,13 +154,14 @@ __device__ __forceinline__ int columns_extreme(int x) {
   return __builtin_amdgcn_readfirstlane(x);
 }
 
-// The sequence with k longer ones before it (in blocks of tokens; the first first where
-// they are equal), for up to 64: bit by bit of the length, from the top, the half of the
-// candidates that holds it.
+// The sequence with k longer ones before it (in units of 128 tokens up to 2^10 of them;
+// the first first where they are equal), for up to 64: bit by bit of the length, from the
+// top, the half of the candidates that holds it.
 __device__ __forceinline__ int nth_longest(const int32_t* __restrict__ lens, int num_seqs, int k, int lane) {
-  constexpr int kBits = 16;
+  constexpr int kBits = 10;
+  constexpr int kLenUnit = 128;
   int len = lane < num_seqs ? lens[lane] : 0;
-  len = len < 0 ? 0 : len / kBlock < (1 << kBits) - 1 ? len / kBlock : (1 << kBits) - 1;
+  len = len < 0 ? 0 : len / kLenUnit < (1 << kBits) - 1 ? len / kLenUnit : (1 << kBits) - 1;
   unsigned long long left = __ballot(lane < num_seqs);
 #pragma unroll
   for (int bit = kBits - 1; bit >= 0; --bit) {
@@ -181,44 +201,45 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
   const int stage_wave = kSplitKv ? 0 : wave;
   const int n = lane & 15;
   const int c = lane >> 4;
-  const int g = pp.group;
+  const int g = pp.group.d;
   // Workgroups are dealt to the XCDs in turn.  Eight units at a time have one XCD each,
   // whose L2 serves their tiles' re-reads; the tiles of the units left over (all of them,
   // with fewer than 8) go to the XCDs in turn.  In a grid that is not resident at once the
   // last tile, which sees the most tokens, goes first, and of up to 64 sequences the longest.
   const int whole_units = pp.units & ~(kXcds - 1);
-  const int whole_blocks = whole_units * pp.tiles;
+  const int whole_blocks = whole_units * pp.tiles.d;
   int tile, unit;
-  const int share = pp.splits > 1 ? (int)blockIdx.x / (pp.tiles * pp.units) : 0;  // of the blocks
-  const int block = (int)blockIdx.x - share * (pp.tiles * pp.units);
+  const int share = pp.splits > 1 ? (int)blockIdx.x / (pp.tiles.d * pp.units) : 0;  // of the blocks
+  const int block = (int)blockIdx.x - share * (pp.tiles.d * pp.units);
   if (block < whole_blocks) {
     const int slot = block / kXcds;
-    tile = slot % pp.tiles;
-    unit = (slot / pp.tiles) * kXcds + block % kXcds;
+    const int eight = pp.tiles.of(slot);
+    tile = slot - eight * pp.tiles.d;
+    unit = eight * kXcds + block % kXcds;
   } else {
     const int at = block - whole_blocks;
-    tile = at / (pp.units - whole_units);
-    unit = whole_units + at - tile * (pp.units - whole_units);
+    tile = pp.rest.of(at);
+    unit = whole_units + at - tile * pp.rest.d;
   }
-  const int kv = unit % pp.hkv;
-  int b = unit / pp.hkv;
+  int b = pp.hkv.of(unit);
+  const int kv = unit - b * pp.hkv.d;
   if (pp.last_first) {
-    tile = pp.tiles - 1 - tile;
-    if (pp.num_seqs <= 64) b = nth_longest(pp.lens, pp.num_seqs, b, lane);
+    tile = pp.tiles.d - 1 - tile;
+    if (pp.num_seqs > 1 && pp.num_seqs <= 64) b = nth_longest(pp.lens, pp.num_seqs, b, lane);
   }
   const int new_tokens = pp.q_lens[b];
   const int nq = new_tokens < pp.max_q_len ? new_tokens : pp.max_q_len;
-  const int first_q = tile * kCols / g;
+  const int first_q = pp.group.of(tile * kCols);
   if (first_q >= nq) return;  // the whole workgroup
   const int row0 = pp.q_starts[b];
   const int seq_len = pp.lens[b] < 0 ? 0 : pp.lens[b];
   const int hist = seq_len - new_tokens;  // position of query 0
-  const int64_t named = (int64_t)pp.max_pages * pp.page_tokens;
+  const int64_t named = (int64_t)pp.max_pages * pp.page_tokens.d;
   int tokens = seq_len < named ? seq_len : (int)named;  // that the table can name
   tokens = tokens < kMostTokens ? tokens : kMostTokens;
   int prefix = pp.prefix_lens != nullptr ? pp.prefix_lens[b] : 0;
   prefix = prefix < 0 ? 0 : prefix < tokens ? prefix : tokens;
-  const size_t row_elems = (size_t)pp.hkv * kHeadDim;
+  const size_t row_elems = (size_t)pp.hkv.d * kHeadDim;
   const int row_bytes = (int)(row_elems * 2);
   const uint16_t* const khead = kc + (size_t)kv * kHeadDim;
   const uint16_t* const vhead = vc + (size_t)kv * kHeadDim;
@@ -230,7 +251,7 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
   // first element of the query (and output) row of the workgroup's column col, -1 if it has none
   auto row_at = [&](int col) -> int64_t {
     const int at = tile * kCols + col;
-    const int qi = at / g;
+    const int qi = pp.group.of(at);
     const int64_t row = (int64_t)row0 + qi;
     return qi < nq && row >= 0 && row < pp.total_q ? (row * pp.hq + kv * g + (at - qi * g)) * kHeadDim : -1;
   };
@@ -247,7 +268,7 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
     const int col = (col_wave * kTiles + ct) * 16 + n;
     const int64_t at = row_at(col);
     const bool valid = at >= 0;
-    const int qi = (tile * kCols + col) / g;
+    const int qi = pp.group.of(tile * kCols + col);
     const int head = kv * g + (tile * kCols + col - qi * g);
     const int64_t row = (int64_t)row0 + qi;
     const int p = hist + qi;
@@ -314,7 +335,8 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
   const int own = gaps ? hist + first_q : INT_MAX;  // position of the workgroup's first row
   __shared__ uint8_t lds_hidden[kCols + kBlock];    // whether own, own + 1, ... are such tokens
   if (gaps) {
-    const int rows = ((tile + 1) * kCols + g - 1) / g < nq ? ((tile + 1) * kCols + g - 1) / g - first_q : nq - first_q;
+    const int past = pp.group.of((tile + 1) * kCols + g - 1);  // the first row that the workgroup has no part of
+    const int rows = (past < nq ? past : nq) - first_q;
     for (int i = tid; i < rows; i += 64 * kWaves) {
       bool seen = false;
       for (int r = i; r < rows && !seen; ++r) {
@@ -378,11 +400,11 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
     const int at = block_at(mine) + (half & 1) * kHalf;
     const int t = token(at);
     if (mine < share_end && at < v_end) {
-      const int j = t / pp.page_tokens;
+      const int j = pp.page_tokens.of(t);
       if (j < pp.max_pages) {
         const int page = pp.block_tables[(size_t)b * pp.max_pages + j];
         if (page >= 0 && page < pp.num_pages) {
-          const int row = page * pp.page_tokens + (t - j * pp.page_tokens);
+          const int row = page * pp.page_tokens.d + (t - j * pp.page_tokens.d);
           const uint32_t edge = ((t < first) | (t + kHalf > own)) && t + kHalf > prefix ? kEdge : 0u;
           halves = (uint32_t)(row / kHalf) << 6 | edge | (uint32_t)(end - t < kHalf ? end - t : kHalf);
         }
@@ -924,12 +946,12 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   pp.window = sc.window;
   pp.max_pages = max_pages_per_seq;
   pp.num_pages = num_pages;
-  pp.page_tokens = d.page_tokens;
+  pp.page_tokens = Divisor(d.page_tokens);
   pp.total_q = total_q;
   pp.max_q_len = max_q_len < total_q ? max_q_len : total_q;
   pp.hq = d.num_q_heads;
-  pp.hkv = d.num_kv_heads;
-  pp.group = g;
+  pp.hkv = Divisor(d.num_kv_heads);
+  pp.group = Divisor(g);
   pp.num_seqs = num_seqs;
   pp.factor = (float)((double)scale * 1.4426950408889634);
   pp.cap_in = sc.softcap > 0.f ? scale / sc.softcap : 0.f;
@@ -979,9 +1001,12 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   pp.o_ws = h->o_ws;
   pp.ml_ws = h->ml_ws;
   const int64_t blocks = split > 0 ? narrow * pp.splits : wide(tiles);
-  if (units > INT32_MAX || blocks > INT32_MAX || cols > kMostTokens) return fail(CTX_ERR_INVALID_ARG, "prefill grid too large");
+  // kMostTokens: indexes past the last stay in 32 bits
+  if (units > kMostTokens || blocks > kMostTokens || cols > kMostTokens)
+    return fail(CTX_ERR_INVALID_ARG, "prefill grid too large");
   pp.units = (int32_t)units;
-  pp.tiles = (int32_t)(blocks / pp.splits / units);
+  pp.tiles = Divisor((int32_t)(blocks / pp.splits / units));
+  pp.rest = Divisor(units % kXcds > 0 ? (int32_t)(units % kXcds) : 1);
   pp.last_first = split == 0 && blocks > 2 * cus;
   const PagedArgs a{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k_pages),
                     static_cast<const uint16_t*>(v_pages), pp, out, (unsigned)blocks,
