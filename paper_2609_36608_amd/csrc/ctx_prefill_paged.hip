@@ -40,10 +40,11 @@
 
 // Bound by vector and matrix work together, at the clock that the power limit leaves: 100
 // requests with 128..512 new tokens over 4,096..12,288 (32/8 heads, 16-token pages) run at
-// 1,045..1,070 TFLOP/s, capped at 870, with slopes at 950, with both at 820; a single prompt
-// of 10,240 tokens at 1,120 with shuffled pages and at 1,212 with pages in order.  A wave
-// holds 16 columns in each of up to 3 tiles, since every K and V fragment read from LDS is
-// then used three times; a fourth would leave no registers (256 at two waves per SIMD).
+// 1,045 TFLOP/s, with slopes at 980, capped at 805, with both at 786, with fp32 outputs at
+// 551; a single prompt of 10,240 tokens at 1,050..1,120 with shuffled pages and at
+// 1,160..1,212 with pages in order.  A wave holds 16 columns in each of up to 3 tiles,
+// since every K and V fragment read from LDS is then used three times; a fourth would
+// leave no registers (256 at two waves per SIMD).
 
 #include <hip/hip_runtime.h>
 

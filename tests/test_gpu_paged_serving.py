@@ -177,3 +177,92 @@ def test_a_step_in_a_graph_follows_its_inputs():
             assert torch.equal(got.view(torch.int16), ref.view(torch.int16))
     del g
     attn.close()
+
+
+def test_sequences_that_share_pages():
+    """Pages of a common beginning in the tables of several sequences."""
+    bt = Batch(11, [600, 90, 333, 64], [20, 3, 40, 1], PAGE, HQ, HKV, gap=1)
+    bt.table[1, :4] = bt.table[0, :4]
+    bt.table[2, :17] = bt.table[0, :17]
+    bt.table[3, :4] = bt.table[2, :4]
+    kc, vc, table, lens = bt.k.to(dev()), bt.v.to(dev()), up_i32(bt.table), up_i32(bt.lens)
+    kw = dict(window=200, prefix=[48, 33, 64, 5], softcap=20.0)
+    sc = AttnScores(20.0, 200, None, up_i32(kw["prefix"]))
+    ref = attention_reference(bt, SCALE, **kw)
+    live = torch.tensor([at is not None for at in bt.row_of()])
+    with DecodeAttention(HQ, HKV, 4, 600, page_tokens=PAGE) as attn:
+        out = torch.empty((bt.rows, HQ, D), device=dev())
+        attn.prefill_paged(bt.q.to(dev()), kc, vc, table, lens, up_i32(bt.starts), up_i32(bt.new), 40, SCALE, out, scores=sc)
+        torch.cuda.synchronize()
+        assert ((out.cpu().double() - ref)[live].abs() <= 9e-5).all()
+        newest = [int(s) + m - 1 for s, m in zip(bt.starts, bt.new)]
+        step = torch.empty((4, HQ, D), device=dev())
+        attn.run_paged(bt.q[newest].to(dev()), kc, vc, table, lens, SCALE, step, scores=sc)
+        torch.cuda.synchronize()
+        assert ((step.cpu().double() - ref[newest]).abs() <= 9e-5).all()
+
+
+def calls_of_a_handle(seed):
+    """A prefill whose rows share their context out and a decode step, both through the workspace."""
+    bt = Batch(seed, [3000, 700, 33], [3, 5, 1], PAGE, HQ, HKV)
+    kc, vc, q = bt.k.to(dev()), bt.v.to(dev()), bt.q.to(dev())
+    table, lens, starts, new = (up_i32(x) for x in (bt.table, bt.lens, bt.starts, bt.new))
+    out, step = torch.empty((bt.rows, HQ, D), device=dev()), torch.empty((3, HQ, D), device=dev())
+    attn = DecodeAttention(HQ, HKV, 3, 30000, page_tokens=PAGE)
+    sc = AttnScores(softcap=25.0, window=2500)
+
+    def prefill(stream=None):
+        attn.prefill_paged(q, kc, vc, table, lens, starts, new, 5, SCALE, out, scores=sc, stream=stream)
+
+    def decode(stream=None):
+        attn.run_paged(q[:3], kc, vc, table, lens, SCALE, step, scores=sc, stream=stream)
+
+    return attn, prefill, decode, out, step
+
+
+def test_two_handles_on_two_streams():
+    handles = [calls_of_a_handle(seed) for seed in (21, 22)]
+    want = []
+    for _, prefill, decode, out, step in handles:
+        prefill()
+        decode()
+        torch.cuda.synchronize()
+        want.append((out.clone(), step.clone()))
+    streams = [torch.cuda.Stream() for _ in handles]
+    for _ in range(5):
+        for _, _, _, out, step in handles:
+            out.fill_(float("nan"))
+            step.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for s, (_, prefill, decode, _, _) in zip(streams, handles):
+                prefill(s)
+                decode(s)
+        torch.cuda.synchronize()
+        for (_, _, _, out, step), (o, d) in zip(handles, want):
+            assert torch.equal(out, o) and torch.equal(step, d)
+    for h in handles:
+        h[0].close()
+
+
+def test_two_graphs_share_a_handle():
+    """Prefill and decode captured into graphs of their own, replayed in turn with eager calls between."""
+    from test_gpu_graphs import capture
+
+    attn, prefill, decode, out, step = calls_of_a_handle(23)
+    prefill()
+    decode()
+    torch.cuda.synchronize()
+    want = out.clone(), step.clone()
+    graphs = capture(prefill), capture(decode)
+    for order in ((0, 1), (1, 0), (0, 0, 1), (1, 1, 0)):
+        out.fill_(float("nan"))
+        step.fill_(float("nan"))
+        for i in order:
+            graphs[i].replay()
+            if order[0]:
+                prefill()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(step, want[1])
+    del graphs
+    attn.close()
