@@ -106,6 +106,7 @@ int ctx_kv_append_run_paged(ctx_decode_attn* handle, const void* q, int64_t q_st
  * the window and the documents are.  The output is the softmax over the seen tokens
  * times their values; a query that sees none gets zeros.
  */
+#define CTX_SCORES_SPLIT_P 1u
 typedef struct {
   float softcap;              /* > 0 (up to 1e38, and scale / softcap too), or 0: no cap */
   int32_t window;             /* > 0, or 0: no window */
@@ -114,6 +115,8 @@ typedef struct {
   const int32_t* doc_starts;  /* int32, the first token of each query's document, one per packed
                                  row (prefill) or sequence (decode), or NULL: 0.  A value above p
                                  (a padding row) leaves the query its prefix alone */
+  uint32_t flags;             /* 0 or CTX_SCORES_SPLIT_P: the prefill with bf16 outputs carries its
+                                 softmax weights as two bf16 terms instead of one */
 } ctx_attn_scores;
 
 /*
@@ -126,8 +129,10 @@ typedef struct {
  *   out     [total_q, Hq, D] of desc.out_dtype, contiguous
  * Arithmetic: fp32 scores and softmax statistics, fp32 accumulation.  With bf16
  * outputs the softmax weights enter the product with V rounded to bf16, and each
- * row is normalised by the sum of the rounded weights; with fp32 outputs as three
- * bf16 terms (24 significant bits).
+ * row is normalised by the sum of the rounded weights (an error of the size of the
+ * outputs' own rounding); CTX_SCORES_SPLIT_P carries them as two bf16 terms (16
+ * significant bits), for a second product with V.  With fp32 outputs they are three
+ * bf16 terms (24 significant bits), whatever the flag.
  * Keys and values that some query of the sequence sees must be finite, their scores
  * too; what no query sees may hold anything.
  * Calls with few rows share a long context out over workgroups that meet in the

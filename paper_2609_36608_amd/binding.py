@@ -25,6 +25,7 @@ CTX_DTYPE_F32 = 1
 HEAD_DIM = 128
 CTX_ROTARY_INTERLEAVED = 1  # ctx_rotary flag: pairs of neighbouring dimensions
 CTX_PREFILL_SPLIT_P = 1  # ctx_prefill_attn_run flag: softmax weights as two bf16 terms
+CTX_SCORES_SPLIT_P = 1  # ctx_attn_scores flag: the same of ctx_prefill_attn_run_paged with bf16 outputs
 CTX_STATIC_SCRATCH_BYTES = 16 << 20  # static workspace of ctx_decode_attn_run_static, per device
 CTX_HBM_SINK_BYTES_PER_WORKGROUP = 64
 CTX_HBM_NONTEMPORAL = 1
@@ -91,7 +92,7 @@ class CtxRotary(ctypes.Structure):
 
 class CtxAttnScores(ctypes.Structure):
     _fields_ = [("softcap", ctypes.c_float), ("window", ctypes.c_int32), ("slopes", ctypes.c_void_p),
-                ("prefix_lens", ctypes.c_void_p), ("doc_starts", ctypes.c_void_p)]
+                ("prefix_lens", ctypes.c_void_p), ("doc_starts", ctypes.c_void_p), ("flags", ctypes.c_uint32)]
 
 
 class RolloutConfig(ctypes.Structure):
@@ -248,10 +249,12 @@ class AttnScores:
     softcap * tanh(s / softcap), less slopes[head] * |p - t|; token t is seen from position p if
     t < prefix_lens[sequence] or max(doc_start, p - window + 1) <= t <= p.  slopes: float32 [Hq],
     prefix_lens: int32 [B], doc_starts: int32, one per packed row (prefill) or sequence (decode);
-    0 and None leave a part out."""
+    0 and None leave a part out.  split_p: the prefill with bf16 outputs carries its softmax weights
+    as two bf16 terms (CTX_SCORES_SPLIT_P) instead of one; the other calls always do, or as three."""
 
-    def __init__(self, softcap: float = 0.0, window: int = 0, slopes=None, prefix_lens=None, doc_starts=None):
-        self.softcap, self.window = softcap, window
+    def __init__(self, softcap: float = 0.0, window: int = 0, slopes=None, prefix_lens=None, doc_starts=None,
+                 split_p: bool = False):
+        self.softcap, self.window, self.split_p = softcap, window, split_p
         self.slopes, self.prefix_lens, self.doc_starts = slopes, prefix_lens, doc_starts
 
 
@@ -272,7 +275,8 @@ def _scores_struct(scores: AttnScores, device: int, num_q_heads: int, seqs: int,
         _need("prefix_lens", prefix, torch.int32, device, (seqs,))
     if docs is not None:
         _need("doc_starts", docs, torch.int32, device, (rows,))
-    return ctypes.byref(CtxAttnScores(scores.softcap, scores.window, _ptr(slopes), _ptr(prefix), _ptr(docs)))
+    return ctypes.byref(CtxAttnScores(scores.softcap, scores.window, _ptr(slopes), _ptr(prefix), _ptr(docs),
+                                      CTX_SCORES_SPLIT_P if scores.split_p else 0))
 
 
 class DecodeAttention:

@@ -181,6 +181,7 @@ constexpr int32_t kMostTokens = 1 << 30;  // in paged caches: rows and positions
   if (sc.softcap > 0.f && !(std::fabs(scale / sc.softcap) <= 1e38f))
     return fail(CTX_ERR_INVALID_ARG, "scale / softcap must be in [-1e38, 1e38]");
   if (sc.window < 0) return fail(CTX_ERR_INVALID_ARG, "window %d < 0", sc.window);
+  if ((sc.flags & ~CTX_SCORES_SPLIT_P) != 0) return fail(CTX_ERR_INVALID_ARG, "unknown score flags 0x%x", sc.flags);
   return CTX_OK;
 }
 

@@ -35,13 +35,14 @@
 //     prefix or to its own position, whichever applies: the same for all tokens of a
 //     row, it does not change the softmax and keeps large logits precise.
 //   * bf16 outputs: weights rounded to bf16 and normalised by the sum of the rounded
-//     ones.  fp32 outputs: three bf16 terms (24 bits), in two tiles per wave, since
-//     three would not leave registers for them.
+//     ones, or, with CTX_SCORES_SPLIT_P, two bf16 terms (16 bits).  fp32 outputs: three
+//     (24 bits).  With more than one, two tiles per wave, since three would not leave
+//     registers for them.
 
 // Bound by vector and matrix work together, at the clock that the power limit leaves: 100
 // requests with 128..512 new tokens over 4,096..12,288 (32/8 heads, 16-token pages) run at
 // 1,045 TFLOP/s, with slopes at 980, capped at 805, with both at 786, with fp32 outputs at
-// 551; a single prompt of 10,240 tokens at 1,050..1,120 with shuffled pages and at
+// 551; with two-term weights at 705, with slopes at 704, capped at 546; a single prompt of 10,240 tokens at 1,050..1,120 with shuffled pages and at
 // 1,160..1,212 with pages in order.  A wave holds 16 columns in each of up to 3 tiles,
 // since every K and V fragment read from LDS is then used three times; a fourth would
 // leave no registers (256 at two waves per SIMD).
@@ -179,8 +180,9 @@ __device__ __forceinline__ int nth_longest(const int32_t* __restrict__ lens, int
   return __builtin_ctzll(__ballot((left >> lane & 1) && before == k));
 }
 
-// kSplit: 0 for wide workgroups, or the waves of a narrow one.  kTiles: 16-column tiles per wave.
-template <typename OutT, int kChange, int kSplit, int kTiles>
+// kTerms: bf16 terms of each softmax weight, 1, 2 (16 bits) or 3 (24).  kSplit: 0 for wide
+// workgroups, or the waves of a narrow one.  kTiles: 16-column tiles per wave.
+template <typename OutT, int kTerms, int kChange, int kSplit, int kTiles>
 __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_per_eu(2))) void prefill_paged_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ kc, const uint16_t* __restrict__ vc, PagedPlan pp,
     OutT* __restrict__ out) {
@@ -189,7 +191,6 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
   constexpr bool kHasBias = (kChange & 1) != 0;
   constexpr bool kHasCap = kChange >= kCap;
   constexpr bool kFarCap = kChange >= kFar;
-  constexpr int kTerms = sizeof(OutT) == 4 ? 3 : 1;
   constexpr int kCols = (kSplitKv ? 1 : kWaves) * kTiles * 16;
   constexpr int kStagers = kSplitKv ? 1 : kWaves;  // waves that stage a block together
   constexpr int kRounds = kHalf / (4 * kStagers);  // loads per thread and half block
@@ -872,37 +873,37 @@ struct PagedArgs {
   hipStream_t stream;
 };
 
-// most tiles per wave: with fp32 outputs three would not leave registers for the terms
-template <typename OutT>
-constexpr int kMostTiles = sizeof(OutT) == 4 ? 2 : 3;
+// most tiles per wave: three would not leave registers for more than one term
+constexpr int most_tiles_of(int terms) { return terms > 1 ? 2 : 3; }
 
-template <typename OutT, int kChange, int kSplit, int kTiles>
+template <typename OutT, int kTerms, int kChange, int kSplit, int kTiles>
 void launch_split(const PagedArgs& a) {
-  hipLaunchKernelGGL((prefill_paged_kernel<OutT, kChange, kSplit, kTiles>), dim3(a.grid), dim3(64 * wg_waves(kSplit)),
-                     0, a.stream, a.q, a.k, a.v, a.plan, static_cast<OutT*>(a.out));
+  hipLaunchKernelGGL((prefill_paged_kernel<OutT, kTerms, kChange, kSplit, kTiles>), dim3(a.grid),
+                     dim3(64 * wg_waves(kSplit)), 0, a.stream, a.q, a.k, a.v, a.plan, static_cast<OutT*>(a.out));
 }
 
-template <typename OutT, int kChange>
+template <typename OutT, int kTerms, int kChange>
 void launch_change(const PagedArgs& a, int split, int tiles) {
-  if (split == 8) return launch_split<OutT, kChange, 8, kMostTiles<OutT>>(a);
-  if (split == 4) return launch_split<OutT, kChange, 4, kMostTiles<OutT>>(a);
-  if (tiles == 1) return launch_split<OutT, kChange, 0, 1>(a);
-  if (tiles == 2) return launch_split<OutT, kChange, 0, 2>(a);
-  launch_split<OutT, kChange, 0, kMostTiles<OutT>>(a);
+  constexpr int kMostTiles = most_tiles_of(kTerms);
+  if (split == 8) return launch_split<OutT, kTerms, kChange, 8, kMostTiles>(a);
+  if (split == 4) return launch_split<OutT, kTerms, kChange, 4, kMostTiles>(a);
+  if (tiles == 1) return launch_split<OutT, kTerms, kChange, 0, 1>(a);
+  if (tiles == 2) return launch_split<OutT, kTerms, kChange, 0, 2>(a);
+  launch_split<OutT, kTerms, kChange, 0, kMostTiles>(a);
 }
 
-template <typename OutT>
+template <typename OutT, int kTerms>
 void launch_paged(const PagedArgs& a, int change, int split, int tiles) {
   if (change == kPlain)
-    launch_change<OutT, kPlain>(a, split, tiles);
+    launch_change<OutT, kTerms, kPlain>(a, split, tiles);
   else if (change == kBias)
-    launch_change<OutT, kBias>(a, split, tiles);
+    launch_change<OutT, kTerms, kBias>(a, split, tiles);
   else if (change == kCap)
-    launch_change<OutT, kCap>(a, split, tiles);
+    launch_change<OutT, kTerms, kCap>(a, split, tiles);
   else if (change == kCapBias)
-    launch_change<OutT, kCapBias>(a, split, tiles);
-  else if constexpr (sizeof(OutT) == 2)
-    change == kFar ? launch_split<OutT, kFar, 0, 1>(a) : launch_split<OutT, kFarBias, 0, 1>(a);
+    launch_change<OutT, kTerms, kCapBias>(a, split, tiles);
+  else if constexpr (kTerms == 1)
+    change == kFar ? launch_split<OutT, kTerms, kFar, 0, 1>(a) : launch_split<OutT, kTerms, kFarBias, 0, 1>(a);
   if (a.plan.splits > 1) {
     const int64_t parts = (int64_t)a.plan.total_q * a.plan.hq;
     hipLaunchKernelGGL((prefill_join_kernel<OutT>), dim3((unsigned)((parts + kJoinWaves - 1) / kJoinWaves)),
@@ -963,7 +964,8 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   const auto grid_of = [&](int64_t wg_cols) { return units * ((cols + wg_cols - 1) / wg_cols); };
   const int64_t cus = h->num_cus;
   // most tokens that a row can see, as far as the host knows
-  const int most_tiles = d.out_dtype == CTX_DTYPE_F32 ? kMostTiles<float> : kMostTiles<uint16_t>;
+  const int terms = d.out_dtype == CTX_DTYPE_F32 ? 3 : (sc.flags & CTX_SCORES_SPLIT_P) != 0 ? 2 : 1;
+  const int most_tiles = most_tiles_of(terms);
   int64_t context = d.max_seq_len;
   if (sc.window > 0 && sc.prefix_lens == nullptr && (int64_t)sc.window + most_tiles * 16 < context)
     context = (int64_t)sc.window + most_tiles * 16;
@@ -973,7 +975,7 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   // waves 42, wide 82).  Not for short contexts, which leave a wave few blocks: 400 fresh
   // tokens 13.5 us wide, 15.8 narrow.
   const int64_t narrow = grid_of(most_tiles * 16);
-  const bool far_cap = d.out_dtype != CTX_DTYPE_F32 && sc.softcap > kFarFrom;
+  const bool far_cap = terms == 1 && sc.softcap > kFarFrom;
   const int split = far_cap || context <= 16 * kBlock || narrow > 2 * cus ? 0 : narrow > cus ? 4 : 8;
   // Wide ones have fewer tiles per wave where there would be too few to fill the chip: one
   // tile as long as all workgroups are resident (three per CU), two (of three) as long as
@@ -1013,10 +1015,12 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
                     static_cast<const uint16_t*>(v_pages), pp, out, (unsigned)blocks,
                     reinterpret_cast<hipStream_t>(stream)};
   const int change = (far_cap ? kFar : sc.softcap > 0.f ? kCap : kPlain) + (sc.slopes != nullptr ? kBias : kPlain);
-  if (d.out_dtype == CTX_DTYPE_F32)
-    launch_paged<float>(a, change, split, tiles);
+  if (terms == 3)
+    launch_paged<float, 3>(a, change, split, tiles);
+  else if (terms == 2)
+    launch_paged<uint16_t, 2>(a, change, split, tiles);
   else
-    launch_paged<uint16_t>(a, change, split, tiles);
+    launch_paged<uint16_t, 1>(a, change, split, tiles);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_fail(e, "kernel launch");
   return CTX_OK;
