@@ -116,7 +116,8 @@ typedef struct {
                                  row (prefill) or sequence (decode), or NULL: 0.  A value above p
                                  (a padding row) leaves the query its prefix alone */
   uint32_t flags;             /* 0 or CTX_SCORES_SPLIT_P: the prefill with bf16 outputs carries its
-                                 softmax weights as two bf16 terms instead of one */
+                                 softmax weights as two bf16 terms instead of one, as it does
+                                 for a softcap above 512 in any case */
 } ctx_attn_scores;
 
 /*

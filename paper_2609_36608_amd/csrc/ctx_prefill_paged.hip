@@ -71,11 +71,15 @@ constexpr int kNowhere = 0x7ffffff0;  // a byte offset past every range
 constexpr int kHeld = 64;   // half blocks whose cache rows a wave holds
 
 // what a kernel changes of the scores
-enum Change { kPlain, kBias, kCap, kCapBias, kFar, kFarBias };  // kFar: a cap far above the scores
+enum Change { kPlain, kBias, kCap, kCapBias };
 
-// Caps from which a score of its own precision counts among bf16 weights too: up to here
-// 2^-23 of the cap, in log2 units, is within 1e-4.  Such a cap hardly changes anything, so
-// these calls have one kernel, of one tile per wave.
+// The cap of one-term weights is 1 - 2 / (e^2y + 1), which loses up to 3.5 * 2^-23 of the cap:
+// the reciprocal, the sum below it and the maximum taken off cost 2^-23 each, exp2 half of
+// that.  A weight is off by as much of itself: 2.1e-4 at this cap, a twentieth of what its
+// rounding may cost (2^-8).  Calls with larger caps take the kernels of two-term weights,
+// whose cap keeps a score's own precision: 16 new tokens over 20,000 29.1 us (30.5 with a
+// cap of 512), 1,024 over 4,000 169 (134).  One-term kernels with that cap, in wide
+// workgroups of one tile alone, took 479 and 155 us.
 constexpr float kFarFrom = 512.f;
 
 // s_waitcnt vmcnt(n) with expcnt and lgkmcnt left open
@@ -190,7 +194,6 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
   constexpr int kWaves = wg_waves(kSplit);
   constexpr bool kHasBias = (kChange & 1) != 0;
   constexpr bool kHasCap = kChange >= kCap;
-  constexpr bool kFarCap = kChange >= kFar;
   constexpr int kCols = (kSplitKv ? 1 : kWaves) * kTiles * 16;
   constexpr int kStagers = kSplitKv ? 1 : kWaves;  // waves that stage a block together
   constexpr int kRounds = kHalf / (4 * kStagers);  // loads per thread and half block
@@ -528,9 +531,8 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
     };
     if constexpr (!kHasCap) {
       each(0.f, [&](float x, float add) __attribute__((always_inline)) { return fmaf(x, pp.factor, add); });
-    } else if constexpr (kTerms == 1 && !kFarCap) {
-      // tanh(y) = 1 - 2 / (e^2y + 1), 2^-23 of the cap off: far below a bf16 weight's
-      // rounding.  (An odd polynomial up to |y| = 1, 7 instructions for 5, and a test
+    } else if constexpr (kTerms == 1) {
+      // tanh(y) = 1 - 2 / (e^2y + 1): off by what kFarFrom allows for.  (An odd polynomial up to |y| = 1, 7 instructions for 5, and a test
       // whether a block's scores all lie there took as long: 100 requests over long
       // contexts 790 TFLOP/s with either; one, with large scores among them, 100 us
       // against 95.)
@@ -900,10 +902,8 @@ void launch_paged(const PagedArgs& a, int change, int split, int tiles) {
     launch_change<OutT, kTerms, kBias>(a, split, tiles);
   else if (change == kCap)
     launch_change<OutT, kTerms, kCap>(a, split, tiles);
-  else if (change == kCapBias)
+  else
     launch_change<OutT, kTerms, kCapBias>(a, split, tiles);
-  else if constexpr (kTerms == 1)
-    change == kFar ? launch_split<OutT, kTerms, kFar, 0, 1>(a) : launch_split<OutT, kTerms, kFarBias, 0, 1>(a);
   if (a.plan.splits > 1) {
     const int64_t parts = (int64_t)a.plan.total_q * a.plan.hq;
     hipLaunchKernelGGL((prefill_join_kernel<OutT>), dim3((unsigned)((parts + kJoinWaves - 1) / kJoinWaves)),
@@ -964,7 +964,9 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   const auto grid_of = [&](int64_t wg_cols) { return units * ((cols + wg_cols - 1) / wg_cols); };
   const int64_t cus = h->num_cus;
   // most tokens that a row can see, as far as the host knows
-  const int terms = d.out_dtype == CTX_DTYPE_F32 ? 3 : (sc.flags & CTX_SCORES_SPLIT_P) != 0 ? 2 : 1;
+  const int terms = d.out_dtype == CTX_DTYPE_F32                                        ? 3
+                    : (sc.flags & CTX_SCORES_SPLIT_P) != 0 || sc.softcap > kFarFrom ? 2
+                                                                                      : 1;
   const int most_tiles = most_tiles_of(terms);
   int64_t context = d.max_seq_len;
   if (sc.window > 0 && sc.prefix_lens == nullptr && (int64_t)sc.window + most_tiles * 16 < context)
@@ -975,8 +977,7 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   // waves 42, wide 82).  Not for short contexts, which leave a wave few blocks: 400 fresh
   // tokens 13.5 us wide, 15.8 narrow.
   const int64_t narrow = grid_of(most_tiles * 16);
-  const bool far_cap = terms == 1 && sc.softcap > kFarFrom;
-  const int split = far_cap || context <= 16 * kBlock || narrow > 2 * cus ? 0 : narrow > cus ? 4 : 8;
+  const int split = context <= 16 * kBlock || narrow > 2 * cus ? 0 : narrow > cus ? 4 : 8;
   // Wide ones have fewer tiles per wave where there would be too few to fill the chip: one
   // tile as long as all workgroups are resident (three per CU), two (of three) as long as
   // about all are (two per CU).  Of 1, 2 and 3 tiles: 1,024 new tokens over 4,000 117, 124
@@ -984,7 +985,7 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   // 600 24, 26 and 32, with up to 300 54, 59 and 46.
   const auto wide = [&](int t) { return grid_of(kWideWaves * t * 16); };
   const int tiles = split > 0             ? most_tiles
-                    : far_cap || wide(1) <= 3 * cus ? 1
+                    : wide(1) <= 3 * cus ? 1
                     : most_tiles > 2 && 4 * wide(2) <= 9 * cus ? 2
                                                                : most_tiles;
   // Where 8-wave workgroups are fewer than the CUs several share a tile's blocks, through
@@ -1014,7 +1015,7 @@ extern "C" int ctx_prefill_attn_run_paged(ctx_decode_attn* h, const void* q, con
   const PagedArgs a{static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k_pages),
                     static_cast<const uint16_t*>(v_pages), pp, out, (unsigned)blocks,
                     reinterpret_cast<hipStream_t>(stream)};
-  const int change = (far_cap ? kFar : sc.softcap > 0.f ? kCap : kPlain) + (sc.slopes != nullptr ? kBias : kPlain);
+  const int change = (sc.softcap > 0.f ? kCap : kPlain) + (sc.slopes != nullptr ? kBias : kPlain);
   if (terms == 3)
     launch_paged<float, 3>(a, change, split, tiles);
   else if (terms == 2)

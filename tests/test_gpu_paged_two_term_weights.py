@@ -91,3 +91,15 @@ def test_fp32_outputs_and_decode_steps_do_not_change():
                                 scores=AttnScores(split_p=s)) for s in (False, True)]
         torch.cuda.synchronize()
     assert torch.equal(outs[0], outs[1]) and torch.equal(steps[0], steps[1])
+
+
+@pytest.mark.parametrize("softcap", [512.5, 1e5])
+@pytest.mark.parametrize("biased", [False, True])
+def test_large_caps_take_two_terms_in_every_kind_of_call(softcap, biased):
+    """Few rows over a long context, shared out, and many over a short one."""
+    for bt, bound in ((Batch(67, [1500, 700], [5, 33], 16, 16, 8), 20000), kind_batch("wide1"), kind_batch("narrow4")):
+        kw = dict(softcap=softcap, slopes=slopes_of(16) if biased else None)
+        ref, spread = attention_reference(bt, SCALE, spread=True, **kw)
+        got, live = run(bt, split_p=False, max_seq_len=bound, **kw)
+        assert excess(got, ref[live], spread[live]) <= 0
+        assert torch.equal(got, run(bt, max_seq_len=bound, **kw)[0])
