@@ -93,11 +93,11 @@ __global__ __launch_bounds__(64 * kWaves) void kv_append_kernel(AppendArgs a) {
   int b, p;
   if (a.q_starts == nullptr) {
     b = j;
-    p = a.lens[b] - 1;
+    p = max(a.lens[b], 0) - 1;
   } else {
     b = row_sequence(a, j, lane);
     if (b < 0) return;
-    p = a.lens[b] - a.q_lens[b] + (j - a.q_starts[b]);
+    p = max(a.lens[b], 0) - a.q_lens[b] + (j - a.q_starts[b]);
   }
   if (p < 0) return;
   // the token's cache row, -1 outside the cache
