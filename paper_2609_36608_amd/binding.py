@@ -218,6 +218,13 @@ def _need(name: str, t, dtype, device: int, shape) -> None:
     raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
 
 
+def _int32(name: str, x) -> int:
+    """x, which ctypes would wrap round where it does not fit."""
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{name} {x} does not fit 32 bits")
+    return x
+
+
 def _stream_ptr(stream, device=None) -> int:
     """hipStream_t of a torch stream (default: the current one of `device`) or a raw handle."""
     import torch
@@ -275,8 +282,11 @@ def _scores_struct(scores: AttnScores, device: int, num_q_heads: int, seqs: int,
         _need("prefix_lens", prefix, torch.int32, device, (seqs,))
     if docs is not None:
         _need("doc_starts", docs, torch.int32, device, (rows,))
-    return ctypes.byref(CtxAttnScores(scores.softcap, scores.window, _ptr(slopes), _ptr(prefix), _ptr(docs),
-                                      CTX_SCORES_SPLIT_P if scores.split_p else 0))
+    s = CtxAttnScores(scores.softcap, _int32("window", scores.window), _ptr(slopes), _ptr(prefix), _ptr(docs),
+                      CTX_SCORES_SPLIT_P if scores.split_p else 0)
+    if s.softcap == 0.0 and scores.softcap != 0.0:  # would be no cap at all
+        raise ValueError(f"softcap {scores.softcap} is below the smallest float32")
+    return ctypes.byref(s)
 
 
 class DecodeAttention:
@@ -478,7 +488,7 @@ class DecodeAttention:
         rc = self.lib.ctx_prefill_attn_run_paged(
             self.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), k_pages.shape[0],
             block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(), q_starts.data_ptr(),
-            q_lens.data_ptr(), b, rows, max_q_len, scale, _scores_struct(scores, dev, self.q_heads, b, rows),
+            q_lens.data_ptr(), b, rows, _int32("max_q_len", max_q_len), scale, _scores_struct(scores, dev, self.q_heads, b, rows),
             out.data_ptr(), self._stream(stream))
         if rc != CTX_OK:
             raise error_for(self.lib, rc)
@@ -509,7 +519,7 @@ class DecodeAttention:
         sp = _stream_ptr(stream)
         rc = self.lib.ctx_prefill_attn_run(self.handle, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
                                            seq_offsets.data_ptr(), seq_lens.data_ptr(), q_starts.data_ptr(),
-                                           q_lens.data_ptr(), b, int(max_q_len), float(scale),
+                                           q_lens.data_ptr(), b, _int32("max_q_len", int(max_q_len)), float(scale),
                                            CTX_PREFILL_SPLIT_P if split_p else 0, out.data_ptr(), sp)
         if rc != CTX_OK:
             raise error_for(self.lib, rc)

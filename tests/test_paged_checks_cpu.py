@@ -13,3 +13,15 @@ def test_unknown_score_flags_are_refused(lib, flags, status):  # noqa: F811
     for rc in (lib.ctx_decode_attn_run_paged_scored(*decode_args(num_seqs=0, **kw).values()),
                lib.ctx_prefill_attn_run_paged(*prefill_args(num_seqs=0, **kw).values())):
         assert rc == (bd.CTX_OK if status is None else status)
+
+
+@pytest.mark.parametrize("window", [2 ** 31, 2 ** 32 + 5, 2 ** 63, -2 ** 31 - 1])
+def test_windows_that_32_bits_would_wrap_are_refused(window):
+    with pytest.raises(ValueError):
+        bd._scores_struct(bd.AttnScores(window=window), 0, 8, 1, 1)
+
+
+@pytest.mark.parametrize("softcap", [1e-46, 5e-324, -1e-50])
+def test_caps_that_a_float_would_make_none_are_refused(softcap):
+    with pytest.raises(ValueError):
+        bd._scores_struct(bd.AttnScores(softcap=softcap), 0, 8, 1, 1)
