@@ -6,6 +6,7 @@ is missing, loading fails with an error that says how to build it.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -238,6 +239,18 @@ def _stream_ptr(stream, device=None) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _allocating_on(stream, device):
+    """Where a call allocates its results: on the stream that it runs on, which then orders them
+    after what held their memory before and before what holds it next."""
+    import torch
+
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream_ptr(stream), device=device)
+    return torch.cuda.stream(stream)
+
+
 class Rotary:
     """What DecodeAttention.append_paged does to queries and keys (ctx_rotary): the norm of each
     head, if weights q_norm / k_norm (bf16 [128]) are given, then the rotation of the first
@@ -422,8 +435,8 @@ class DecodeAttention:
         slots of each sequence's last q_lens[b] of seq_lens[b] tokens (rows q_starts[b] ..; without
         q_starts / q_lens row b is the newest token of sequence b), and q [rows, Hq, D], if given, to
         q_out; q and k are normed and rotated as `rotary` says.  k, v and q may be slices of wider
-        rows (heads and dimensions contiguous).  Returns q_out (if None, allocated on the current
-        stream; without q None)."""
+        rows (heads and dimensions contiguous).  Returns q_out (if None, allocated on the stream
+        that the call runs on; without q None)."""
         import torch
 
         if self.handle is None:
@@ -436,7 +449,8 @@ class DecodeAttention:
         if q is not None:
             q_stride = self._row_stride("q", q, rows, self.q_heads)
             if q_out is None:
-                q_out = torch.empty((rows, self.q_heads, HEAD_DIM), dtype=torch.bfloat16, device=q.device)
+                with _allocating_on(stream, q.device):
+                    q_out = torch.empty((rows, self.q_heads, HEAD_DIM), dtype=torch.bfloat16, device=q.device)
             else:
                 _need("q_out", q_out, torch.bfloat16, dev, (rows, self.q_heads, HEAD_DIM))
         elif q_out is not None:
@@ -584,7 +598,8 @@ def opd_loss(logits, tokens, old_logp, teacher_logp, mask, seq_starts, params: O
     old_logp / teacher_logp float32 [N], mask uint8 [N], seq_starts int32 [B + 1].
     Returns a dict of device tensors: loss [1], token_logp, token_weight,
     token_loss [N] and, with grad=True, grad_logits bf16 [N, vocab].  Tensors
-    given in `out` under those names are written in place (no allocation)."""
+    given in `out` under those names are written in place (no allocation); the others
+    are allocated on the stream that the call runs on."""
     import torch
 
     lib = load_library()
@@ -614,7 +629,8 @@ def opd_loss(logits, tokens, old_logp, teacher_logp, mask, seq_starts, params: O
     def buf(name, shape, dtype):
         t = out.get(name)
         if t is None:
-            return torch.empty(shape, dtype=dtype, device=dev)
+            with _allocating_on(stream, dev):
+                return torch.empty(shape, dtype=dtype, device=dev)
         if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != dev:
             raise ValueError(f"out[{name!r}] must be a contiguous {dtype} tensor of shape {tuple(shape)}")
         return t
@@ -626,7 +642,8 @@ def opd_loss(logits, tokens, old_logp, teacher_logp, mask, seq_starts, params: O
     if grad:
         g = out.get("grad_logits")
         if g is None:  # rows padded to a multiple of 8 elements (16-byte chunks)
-            g = torch.empty((n, (vocab + 7) // 8 * 8), dtype=torch.bfloat16, device=dev)
+            with _allocating_on(stream, dev):
+                g = torch.empty((n, (vocab + 7) // 8 * 8), dtype=torch.bfloat16, device=dev)
         elif (g.dtype != torch.bfloat16 or g.dim() != 2 or g.shape[0] != n or g.stride(1) != 1
               or g.shape[1] < vocab or g.device != dev):
             raise ValueError(f"out['grad_logits'] must be bf16 [N, >= {vocab}] with unit column stride on {dev}")
