@@ -319,7 +319,7 @@ extern "C" int ctx_kv_append_run_paged(ctx_decode_attn* h, const void* q, int64_
   // those that move more than the 256 MiB last-level cache read past them too: 30,600 rows
   // of 32/8 heads 156 us, 146 and 142.  (Smaller calls find in it what the projection
   // has just written: 9,600 rows and their prefill 192 us, 206 with both.)
-  const int64_t moved = (int64_t)a.rows * (a.hq + 2 * a.hkv) * kHeadDim * 2 * 2;
+  const int64_t moved = (int64_t)a.rows * ((a.q != nullptr ? a.hq : 0) + 2 * a.hkv) * kHeadDim * 2 * 2;
   if ((int64_t)a.rows < 11 * (int64_t)h->num_cus)
     launch_append<kWaves, kCached>(a, norm, interleaved, s);
   else if (moved <= (int64_t)256 << 20)
