@@ -138,8 +138,13 @@ typedef struct {
  * too; what no query sees may hold anything.
  * Calls with few rows share a long context out over workgroups that meet in the
  * handle's workspace: as for ctx_decode_attn_run, calls that may overlap need separate
- * handles.  num_seqs, total_q, max_q_len, the window, desc and the device's CU count choose the kernel; the
- * same request alone and in a batch may differ by the rounding of its weights.
+ * handles.
+ * The kernel, and with it the order of sums and the roundings of weights, is chosen by num_seqs,
+ * total_q, max_q_len, desc, the device's CU count and, of the scores, by the flags, the window, whether
+ * prefix_lens and slopes are given, and the softcap (none, up to 512, above; a cap so large that
+ * scale / softcap is below the smallest normal float counts as none).  So the same request alone and
+ * in a batch may differ by those roundings.  desc.max_seq_len counts as the longest context: on a
+ * handle for far longer ones, calls of a few rows over short contexts take 2 to 3 times as long.
  * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, ALIGNMENT, HIP.
  */
 int ctx_prefill_attn_run_paged(ctx_decode_attn* handle, const void* q, const void* k_pages, const void* v_pages,

@@ -4,8 +4,8 @@
 //
 // Per packed row (one new token): Hq query, Hkv key and Hkv value heads of 128
 // bf16 are read once and written once, so the work is bound by HBM for many rows
-// (30,600 rows of 32/8 heads 136.8 us, 5.5 TB/s: the copy rate) and by latency for a
-// few (4 rows 4.3 us, 256 5.8).
+// (30,629 rows of 32/8 heads 136 us, 5.5 TB/s: the copy rate) and by latency for a
+// few (4 rows of 16/8 heads 4.0 us, 256 of 32/8 5.6).
 //
 //   * 16 lanes hold one head, 8 dimensions (16 bytes) each; a wave instruction
 //     moves 4 heads.  A row's heads are numbered queries, keys, values; which of
@@ -316,8 +316,9 @@ extern "C" int ctx_kv_append_run_paged(ctx_decode_attn* h, const void* q, int64_
   // a workgroup.  In a graph, 4 waves and 1 per row of 32/8 heads: 64 rows 4.6 and 10.0 us,
   // 1,000 8.7 and 13.6, 2,500 14.0 and 15.4, 3,000 15.4 and 15.8, 3,500 20.2 and 17.7, 4,100
   // 24.0 and 19.4; of 16/8 heads 3,000 12.6 and 12.3.  Large calls write past the caches, and
-  // those that move more than the 256 MiB last-level cache read past them too: 30,600 rows
-  // of 32/8 heads 156 us, 146 and 142.  (Smaller calls find in it what the projection
+  // those that move more than the 256 MiB last-level cache read past them too: 30,629 rows
+  // of 32/8 heads 154 us with neither, 145 with the first, 136 with both; 20,479 of 28/4 77,
+  // 74 and 70.  (Smaller calls find in it what the projection
   // has just written: 9,600 rows and their prefill 192 us, 206 with both.)
   const int64_t moved = (int64_t)a.rows * ((a.q != nullptr ? a.hq : 0) + 2 * a.hkv) * kHeadDim * 2 * 2;
   if ((int64_t)a.rows < 11 * (int64_t)h->num_cus)
