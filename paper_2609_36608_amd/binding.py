@@ -247,7 +247,8 @@ def _allocating_on(stream, device):
     if stream is None:
         return contextlib.nullcontext()
     if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(_stream_ptr(stream), device=device)
+        ptr = _stream_ptr(stream)  # 0, the default stream's, would make ExternalStream a stream of its own
+        stream = torch.cuda.ExternalStream(ptr, device=device) if ptr else torch.cuda.default_stream(device)
     return torch.cuda.stream(stream)
 
 

@@ -39,6 +39,19 @@ def test_append(raw):
         assert given_away(lambda: attn.append_paged(*args, q=q, **rows))  # its own stream's, in order
 
 
+def test_the_default_stream_by_its_handle():
+    bt = Batch(5, [20, 5], [20, 5], 16, 8, 2)
+    q, k, v = (randn(bt.g, (bt.rows, h, D)).to(dev()) for h in (8, 2, 2))
+    args = k, v, bt.k.to(dev()), bt.v.to(dev()), up_i32(bt.table), up_i32(bt.lens)
+    rows = dict(q_starts=up_i32(bt.starts), q_lens=up_i32(bt.new))
+    assert torch.cuda.default_stream().cuda_stream == 0
+    torch.cuda.synchronize()
+    with DecodeAttention(8, 2, 2, 32, page_tokens=16) as attn:
+        assert given_away(lambda: attn.append_paged(*args, q=q, stream=0, **rows))
+        with torch.cuda.stream(torch.cuda.Stream()):
+            assert not given_away(lambda: attn.append_paged(*args, q=q, stream=0, **rows))
+
+
 def test_opd_loss():
     n, vocab = 64, 40000  # a gradient too large for a block of the allocator's small ones
     logits = torch.randn((n, vocab), device=dev()).to(torch.bfloat16)
