@@ -76,7 +76,8 @@ enum Change { kPlain, kBias, kCap, kCapBias };
 // The cap of one-term weights is 1 - 2 / (e^2y + 1), which loses up to 3.5 * 2^-23 of the cap:
 // the reciprocal, the sum below it and the maximum taken off cost 2^-23 each, exp2 half of
 // that.  A weight is off by as much of itself: 2.1e-4 at this cap, a twentieth of what its
-// rounding may cost (2^-8).  Calls with larger caps take the kernels of two-term weights,
+// rounding may cost (2^-8).  (Where slopes below zero make the maximum larger than the cap,
+// taking it off costs 2^-24 of it: a bias of 10,000 is 6e-4.)  Calls with larger caps take the kernels of two-term weights,
 // whose cap keeps a score's own precision: 16 new tokens over 20,000 29.1 us (30.5 with a
 // cap of 512), 1,024 over 4,000 169 (134).  One-term kernels with that cap, in wide
 // workgroups of one tile alone, took 479 and 155 us.
@@ -534,10 +535,10 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
     if constexpr (!kHasCap) {
       each(0.f, [&](float x, float add) __attribute__((always_inline)) { return fmaf(x, pp.factor, add); });
     } else if constexpr (kTerms == 1) {
-      // tanh(y) = 1 - 2 / (e^2y + 1): off by what kFarFrom allows for.  (An odd polynomial up to |y| = 1, 7 instructions for 5, and a test
-      // whether a block's scores all lie there took as long: 100 requests over long
-      // contexts 790 TFLOP/s with either; one, with large scores among them, 100 us
-      // against 95.)
+      // tanh(y) = 1 - 2 / (e^2y + 1): off by what kFarFrom allows for.  (An odd polynomial
+      // up to |y| = 1, 7 instructions for 5, and a test whether a block's scores all lie
+      // there took as long: 100 requests over long contexts 790 TFLOP/s with either; one,
+      // with large scores among them, 100 us against 95.)
       each(pp.cap_out, [&](float x, float add) __attribute__((always_inline)) {
         return fmaf(__builtin_amdgcn_rcpf(fast_exp2(x * pp.cap_in2) + 1.0f), -2.0f * pp.cap_out, add);
       });
