@@ -45,6 +45,9 @@ EXPORTS = (
     "ctx_prefill_attn_run_paged",
     "ctx_decode_attn_run_paged_scored",
     "ctx_opd_loss_run",
+    "ctx_token_logprob_workspace",
+    "ctx_token_logprob_run",
+    "ctx_token_logprob_grad_run",
     "ctx_rollout_simulate",
     "ctx_rollout_simulate_engine",
     "ctx_hbm_read",
@@ -158,6 +161,15 @@ def load_library(path: str | None = None):
     lib.ctx_opd_loss_run.argtypes = [vp, ctypes.c_int64, i32, vp, vp, vp, vp, vp, i32, i32,
                                      ctypes.POINTER(OpdParams), vp, vp, vp, vp, vp, ctypes.c_int64, vp]
     lib.ctx_opd_loss_run.restype = ctypes.c_int
+    size_t, i64, f32 = ctypes.c_size_t, ctypes.c_int64, ctypes.c_float
+    lib.ctx_token_logprob_workspace.argtypes = [ctypes.c_int, i32, i32, i32, ctypes.POINTER(size_t)]
+    lib.ctx_token_logprob_workspace.restype = ctypes.c_int
+    lib.ctx_token_logprob_run.argtypes = [vp, ctypes.c_int, i64, i32, vp, i32, vp, i32, f32, i32, vp, vp, vp, vp, vp, vp,
+                                          size_t, vp]
+    lib.ctx_token_logprob_run.restype = ctypes.c_int
+    lib.ctx_token_logprob_grad_run.argtypes = [vp, ctypes.c_int, i64, i32, vp, i32, vp, i32, f32, vp, vp, vp, vp, vp, i64,
+                                               vp]
+    lib.ctx_token_logprob_grad_run.restype = ctypes.c_int
     lib.ctx_rollout_simulate.argtypes = [ctypes.POINTER(RolloutConfig), vp, vp, vp, vp, vp, vp]
     lib.ctx_rollout_simulate.restype = ctypes.c_int
     lib.ctx_rollout_simulate_engine.argtypes = [ctypes.POINTER(RolloutConfig), ctypes.POINTER(RolloutEngine), vp, vp,
@@ -658,6 +670,149 @@ def opd_loss(logits, tokens, old_logp, teacher_logp, mask, seq_starts, params: O
     if rc != CTX_OK:
         raise error_for(lib, rc)
     return res
+
+
+def _logits_rows(logits, name: str = "logits"):
+    """dtype code, rows, columns and row stride of a matrix of logits."""
+    import torch
+
+    if logits.dtype is not torch.bfloat16 and logits.dtype is not torch.float32:
+        raise TypeError(f"{name} must be bfloat16 or float32, got {logits.dtype}")
+    if not logits.is_cuda:
+        raise ValueError(f"{name} must be on a cuda device")
+    if logits.dim() != 2 or logits.stride(1) != 1:
+        raise ValueError(f"{name} must be [N, V] with unit column stride")
+    rows, vocab = logits.shape
+    # the stride of a single row says nothing
+    stride = logits.stride(0) if rows > 1 else (vocab + 7) // 8 * 8
+    return _dtype_code(logits.dtype), rows, vocab, stride
+
+
+def _logit_tokens(tokens, rows: int, device: int) -> int:
+    """Given tokens per row."""
+    import torch
+
+    if tokens is None:
+        return 0
+    if tokens.dim() == 1:
+        _need("tokens", tokens, torch.int32, device, (rows,))
+        return 1
+    _need("tokens", tokens, torch.int32, device, (rows, tokens.shape[-1]))
+    return tokens.shape[1]
+
+
+def _scale_of(temperature: float) -> float:
+    if not temperature > 0:
+        raise ValueError(f"temperature must be positive, got {temperature}")
+    return 1.0 / temperature
+
+
+def _on_current(device: int, what: str) -> None:
+    import torch
+
+    if torch.cuda.current_device() != device:
+        raise ValueError(f"{what} on cuda:{device}, which is not the current device")
+
+
+def token_logprobs(logits, tokens=None, mask=None, temperature: float = 1.0, top: int = 0, entropy: bool = True,
+                   out: dict | None = None, workspace=None, stream=None) -> dict:
+    """Log probabilities of given tokens under softmax(logits / temperature), its entropy and the
+    `top` largest logits (ctx_token_logprob_run).
+
+    logits bf16 or float32 [N, V] (rows may be views of wider ones, a multiple of 16 bytes apart),
+    tokens int32 [N] or [N, M] (M up to 64; below 0: none), mask uint8 [N] (0: the row is not read).
+    Returns a dict of device tensors: token_logp float32 like tokens, entropy [N] (with entropy=True),
+    top_tokens int32 and top_logp [N, top] (the lowest column first among equal logits, -1 where there
+    is none) and stats [N, 2], which token_logprobs_grad takes.  Tensors given in `out` under those
+    names are written in place; the others, and the workspace of a call on few rows (uint8), are
+    allocated on the stream that the call runs on.  Calls that may overlap need a workspace each."""
+    import torch
+
+    lib = load_library()
+    code, n, vocab, stride = _logits_rows(logits)
+    dev, index = logits.device, logits.get_device()
+    _on_current(index, "logits")
+    m = _logit_tokens(tokens, n, index)
+    if mask is not None:
+        _need("mask", mask, torch.uint8, index, (n,))
+    out = out or {}
+
+    def buf(name, shape, dtype):
+        t = out.get(name)
+        if t is None:
+            return torch.empty(shape, dtype=dtype, device=dev)
+        _need(f"out[{name!r}]", t, dtype, index, shape)
+        return t
+
+    nbytes = ctypes.c_size_t()
+    top = _int32("top", top)
+    if (rc := lib.ctx_token_logprob_workspace(code, _int32("vocab", vocab), n, top, ctypes.byref(nbytes))) != CTX_OK:
+        raise error_for(lib, rc)
+    with _allocating_on(stream, dev):
+        res = {"stats": buf("stats", (n, 2), torch.float32)}
+        if m > 0:
+            res["token_logp"] = buf("token_logp", tokens.shape, torch.float32)
+        if entropy:
+            res["entropy"] = buf("entropy", (n,), torch.float32)
+        if top > 0:
+            res["top_tokens"] = buf("top_tokens", (n, top), torch.int32)
+            res["top_logp"] = buf("top_logp", (n, top), torch.float32)
+        size = nbytes.value
+        if workspace is None:
+            workspace = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
+        else:
+            _need("workspace", workspace, torch.uint8, index, (workspace.numel(),))
+    rc = lib.ctx_token_logprob_run(
+        logits.data_ptr(), code, stride, vocab, _ptr(tokens) if m > 0 else None, m, _ptr(mask), n, _scale_of(temperature), top,
+        _ptr(res.get("token_logp")), _ptr(res.get("entropy")), res["stats"].data_ptr(), _ptr(res.get("top_tokens")),
+        _ptr(res.get("top_logp")), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream, dev))
+    if rc != CTX_OK:
+        raise error_for(lib, rc)
+    return res
+
+
+def token_logprobs_grad(logits, tokens, result: dict, grad_logp, grad_entropy=None, mask=None, temperature: float = 1.0,
+                        out=None, stream=None):
+    """Gradient by the logits of sum(grad_logp * token_logp) + sum(grad_entropy * entropy)
+    (ctx_token_logprob_grad_run); result: what token_logprobs returned for the same logits, mask and
+    temperature.  tokens may be others than that call's (its top_tokens, for instance, with grad_logp
+    the gradient of top_logp); grad_logp float32 like tokens, both None without any.  Returns
+    grad_logits [N, V] of the logits' type (`out`, or allocated on the stream that the call runs on,
+    its rows padded to 16 bytes)."""
+    import torch
+
+    lib = load_library()
+    code, n, vocab, stride = _logits_rows(logits)
+    dev, index = logits.device, logits.get_device()
+    _on_current(index, "logits")
+    m = _logit_tokens(tokens, n, index)
+    if (grad_logp is None) != (tokens is None):
+        raise ValueError("tokens and grad_logp go together")
+    if m > 0:
+        _need("grad_logp", grad_logp, torch.float32, index, tokens.shape)
+    if mask is not None:
+        _need("mask", mask, torch.uint8, index, (n,))
+    _need("result['stats']", result["stats"], torch.float32, index, (n, 2))
+    h = None
+    if grad_entropy is not None:
+        h = result.get("entropy")
+        if h is None:
+            raise ValueError("grad_entropy needs the entropy of the forward call")
+        _need("result['entropy']", h, torch.float32, index, (n,))
+        _need("grad_entropy", grad_entropy, torch.float32, index, (n,))
+    if out is None:
+        with _allocating_on(stream, dev):
+            grad = torch.empty((n, (vocab + 7) // 8 * 8), dtype=logits.dtype, device=dev)
+        out = grad[:, :vocab]
+    elif out.dtype != logits.dtype or out.shape != logits.shape or out.get_device() != index or out.stride(1) != 1:
+        raise ValueError(f"out must be {logits.dtype} {list(logits.shape)} with unit column stride on {dev}")
+    rc = lib.ctx_token_logprob_grad_run(
+        logits.data_ptr(), code, stride, vocab, _ptr(tokens) if m > 0 else None, m, _ptr(mask), n, _scale_of(temperature),
+        result["stats"].data_ptr(), _ptr(h), _ptr(grad_logp) if m > 0 else None, _ptr(grad_entropy), out.data_ptr(),
+        _logits_rows(out, "out")[3], _stream_ptr(stream, dev))
+    if rc != CTX_OK:
+        raise error_for(lib, rc)
+    return out
 
 
 def _rollout_outputs(n, turns):
