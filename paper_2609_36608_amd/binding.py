@@ -44,6 +44,11 @@ EXPORTS = (
     "ctx_kv_append_run_paged",
     "ctx_prefill_attn_run_paged",
     "ctx_decode_attn_run_paged_scored",
+    "ctx_kv_fork_run_paged",
+    "ctx_kv_resize_workspace",
+    "ctx_kv_resize_run_paged",
+    "ctx_kv_copy_run_paged",
+    "ctx_kv_compact_run_paged",
     "ctx_opd_loss_run",
     "ctx_token_logprob_workspace",
     "ctx_token_logprob_run",
@@ -162,6 +167,16 @@ def load_library(path: str | None = None):
                                      ctypes.POINTER(OpdParams), vp, vp, vp, vp, vp, ctypes.c_int64, vp]
     lib.ctx_opd_loss_run.restype = ctypes.c_int
     size_t, i64, f32 = ctypes.c_size_t, ctypes.c_int64, ctypes.c_float
+    lib.ctx_kv_fork_run_paged.argtypes = [vp, vp, i32, vp, i32, vp, vp, i32, vp]
+    lib.ctx_kv_fork_run_paged.restype = ctypes.c_int
+    lib.ctx_kv_resize_workspace.argtypes = [i32, i32]
+    lib.ctx_kv_resize_workspace.restype = size_t
+    lib.ctx_kv_resize_run_paged.argtypes = [vp, vp, i32, vp, vp, i32, vp, i32, vp, vp, vp, size_t, vp]
+    lib.ctx_kv_resize_run_paged.restype = ctypes.c_int
+    lib.ctx_kv_copy_run_paged.argtypes = [vp, vp, vp, i32, vp, i32, vp]
+    lib.ctx_kv_copy_run_paged.restype = ctypes.c_int
+    lib.ctx_kv_compact_run_paged.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, i32, i32, vp, vp]
+    lib.ctx_kv_compact_run_paged.restype = ctypes.c_int
     lib.ctx_token_logprob_workspace.argtypes = [ctypes.c_int, i32, i32, i32, ctypes.POINTER(size_t)]
     lib.ctx_token_logprob_workspace.restype = ctypes.c_int
     lib.ctx_token_logprob_run.argtypes = [vp, ctypes.c_int, i64, i32, vp, i32, vp, i32, f32, i32, vp, vp, vp, vp, vp, vp,
@@ -520,6 +535,116 @@ class DecodeAttention:
         if rc != CTX_OK:
             raise error_for(self.lib, rc)
         return out
+
+    def _check_rows(self, block_tables, seq_lens, page_refs) -> int:
+        """Rows of a block table whose pages are counted."""
+        import torch
+
+        if self.handle is None:
+            raise RuntimeError("handle is closed")
+        seqs = seq_lens.shape[0]
+        _need("seq_lens", seq_lens, torch.int32, self.device, (seqs,))
+        _need("block_tables", block_tables, torch.int32, self.device, (seqs, block_tables.shape[-1]))
+        _need("page_refs", page_refs, torch.int32, self.device, (page_refs.shape[0],))
+        return seqs
+
+    def fork_pages(self, block_tables, seq_lens, page_refs, parents, stream=None):
+        """Fork rows of a block table (ctx_kv_fork_run_paged): row b and seq_lens[b] become those of
+        row parents[b] (-1: row b stays as it is), whose pages both then hold; page_refs int32 [pages]
+        counts the rows that hold each page.  All three are written in place."""
+        import torch
+
+        seqs = self._check_rows(block_tables, seq_lens, page_refs)
+        _need("parents", parents, torch.int32, self.device, (seqs,))
+        rc = self.lib.ctx_kv_fork_run_paged(
+            self.handle, block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(), seqs, parents.data_ptr(),
+            page_refs.data_ptr(), page_refs.shape[0], self._stream(stream))
+        if rc != CTX_OK:
+            raise error_for(self.lib, rc)
+
+    def resize_pages(self, block_tables, seq_lens, new_lens, page_refs, granted=None, copies=None, workspace=None,
+                     stream=None):
+        """Change the lengths of the rows of a block table from seq_lens to new_lens
+        (ctx_kv_resize_run_paged): pages are given back, or the lowest free ones taken, in the order of
+        rows, and a last page that other rows hold too is replaced where the row grows in it.  Writes
+        block_tables and page_refs in place; returns granted int32 [B], the lengths from now on
+        (seq_lens[b] where the free pages did not suffice; may be seq_lens itself), and copies
+        int32 [B, 2], the pages that copy_pages has to copy in each layer's caches.  Those not
+        given, and the workspace (uint8), are allocated on the stream that the call runs on."""
+        import torch
+
+        seqs = self._check_rows(block_tables, seq_lens, page_refs)
+        pages, dev = page_refs.shape[0], seq_lens.device
+        _need("new_lens", new_lens, torch.int32, self.device, (seqs,))
+        if granted is not None:
+            _need("granted", granted, torch.int32, self.device, (seqs,))
+        if copies is not None:
+            _need("copies", copies, torch.int32, self.device, (seqs, 2))
+        if workspace is not None:
+            _need("workspace", workspace, torch.uint8, self.device, (workspace.numel(),))
+        with _allocating_on(stream, dev):
+            if granted is None:
+                granted = torch.empty((seqs,), dtype=torch.int32, device=dev)
+            if copies is None:
+                copies = torch.empty((seqs, 2), dtype=torch.int32, device=dev)
+            if workspace is None:
+                workspace = torch.empty(self.lib.ctx_kv_resize_workspace(seqs, pages), dtype=torch.uint8, device=dev)
+        rc = self.lib.ctx_kv_resize_run_paged(
+            self.handle, block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(), new_lens.data_ptr(), seqs,
+            page_refs.data_ptr(), pages, granted.data_ptr(), copies.data_ptr(), workspace.data_ptr(), workspace.numel(),
+            self._stream(stream))
+        if rc != CTX_OK:
+            raise error_for(self.lib, rc)
+        return granted, copies
+
+    def _check_caches(self, k_pages, v_pages):
+        import torch
+
+        pages = (k_pages.shape[0], self.page_tokens, self.kv_heads, HEAD_DIM)
+        _need("k_pages", k_pages, torch.bfloat16, self.device, pages)
+        _need("v_pages", v_pages, torch.bfloat16, self.device, pages)
+
+    def copy_pages(self, k_pages, v_pages, copies, stream=None):
+        """Copy whole pages of a layer's caches (ctx_kv_copy_run_paged): page copies[i, 0] to
+        copies[i, 1]; -1: nothing."""
+        import torch
+
+        if self.handle is None:
+            raise RuntimeError("handle is closed")
+        self._check_caches(k_pages, v_pages)
+        _need("copies", copies, torch.int32, self.device, (copies.shape[0], 2))
+        rc = self.lib.ctx_kv_copy_run_paged(self.handle, k_pages.data_ptr(), v_pages.data_ptr(), k_pages.shape[0],
+                                            copies.data_ptr(), copies.shape[0], self._stream(stream))
+        if rc != CTX_OK:
+            raise error_for(self.lib, rc)
+
+    def compact_paged(self, k_pages, v_pages, block_tables, seq_lens, q_starts, q_lens, keep, keep_lens, new_lens=None,
+                      stream=None):
+        """Move the kept tokens of each sequence together (ctx_kv_compact_run_paged): of its last
+        q_lens[b] tokens those that keep [rows] lists, rising, in rows q_starts[b] .. q_starts[b] +
+        keep_lens[b] - 1.  Returns new_lens int32 [B], the sequences' lengths without the others (if
+        None, allocated on the stream that the call runs on)."""
+        import torch
+
+        if self.handle is None:
+            raise RuntimeError("handle is closed")
+        dev, seqs, rows = self.device, seq_lens.shape[0], keep.shape[0]
+        self._check_pages(k_pages, v_pages, block_tables, seqs)
+        for name, t in (("seq_lens", seq_lens), ("q_starts", q_starts), ("q_lens", q_lens), ("keep_lens", keep_lens)):
+            _need(name, t, torch.int32, dev, (seqs,))
+        _need("keep", keep, torch.int32, dev, (rows,))
+        if new_lens is None:
+            with _allocating_on(stream, seq_lens.device):
+                new_lens = torch.empty((seqs,), dtype=torch.int32, device=seq_lens.device)
+        else:
+            _need("new_lens", new_lens, torch.int32, dev, (seqs,))
+        rc = self.lib.ctx_kv_compact_run_paged(
+            self.handle, k_pages.data_ptr(), v_pages.data_ptr(), k_pages.shape[0], block_tables.data_ptr(),
+            block_tables.shape[1], seq_lens.data_ptr(), q_starts.data_ptr(), q_lens.data_ptr(), keep.data_ptr(),
+            keep_lens.data_ptr(), seqs, rows, new_lens.data_ptr(), self._stream(stream))
+        if rc != CTX_OK:
+            raise error_for(self.lib, rc)
+        return new_lens
 
     def prefill(self, q, k_cache, v_cache, seq_offsets, seq_lens, q_starts, q_lens, max_q_len: int,
                 scale: float, out, stream=None, split_p: bool = False):

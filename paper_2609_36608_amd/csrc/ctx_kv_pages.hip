@@ -1,0 +1,444 @@
+// ctx_kv_pages.hip -- the pages of paged caches for gfx950 (MI355X): forked, grown, trimmed
+// and freed rows of a block table with counts of the pages' use, and the copies and
+// compaction of the data, behind the C ABI declared in include/ctx_kv_pages.h.
+//
+//   * Counts change by integer atomics, whose order does not matter; pages are handed out
+//     the lowest first, by a prefix sum over the rows' needs and one over the free
+//     pages, so that what a call does depends on its inputs alone.  (A stack of free
+//     pages would need no pass over the counts, but its order would follow that of the
+//     atomics.)
+//   * A resize takes three launches: the pages given back (a workgroup per row), the needs
+//     and the free pages (one workgroup: 4 bytes a page, read once or twice from L2), and
+//     the tables (a workgroup per row).
+//   * Compaction is in place.  A token moves to a place no later than its own, so the
+//     places that the first i tokens go to hold, of what is still needed, only these
+//     tokens themselves: a workgroup takes one head of one sequence's keys or values
+//     through blocks of tokens in order, and writes a block once all of it has been read.
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "ctx_attn_common.h"
+#include "ctx_kv_pages.h"
+
+namespace {
+
+struct Rows {
+  int32_t* tables;
+  int32_t max_pages, page_tokens, num_seqs;
+  int32_t* refs;
+  int32_t num_pages;
+};
+
+__device__ __forceinline__ int64_t clipped(const Rows& r, int32_t len) {
+  const int64_t most = (int64_t)r.max_pages * r.page_tokens;
+  return len < 0 ? 0 : len < most ? len : most;
+}
+__device__ __forceinline__ int pages_of(const Rows& r, int64_t len) {
+  return (int)((len + r.page_tokens - 1) / r.page_tokens);
+}
+__device__ __forceinline__ bool is_page(const Rows& r, int32_t page) { return page >= 0 && page < r.num_pages; }
+__device__ __forceinline__ void count(const Rows& r, int32_t page, int by) {
+  if (is_page(r, page)) atomicAdd(r.refs + page, by);
+}
+
+// ------------------------------------------------------------ fork
+
+constexpr int kRowThreads = 256;
+
+__device__ __forceinline__ bool forks(const int32_t* parents, int num_seqs, int b) {
+  const int p = parents[b];
+  return p >= 0 && p < num_seqs && p != b;
+}
+
+// One workgroup per row.  A row is written only by its own workgroup, and no row that is
+// written is another's parent.
+__global__ __launch_bounds__(kRowThreads) void fork_kernel(Rows r, int32_t* lens, const int32_t* __restrict__ parents) {
+  const int b = blockIdx.x;
+  if (!forks(parents, r.num_seqs, b)) return;
+  const int p = parents[b];
+  if (forks(parents, r.num_seqs, p)) return;
+  const int32_t len = lens[p];
+  const int had = pages_of(r, clipped(r, lens[b])), get = pages_of(r, clipped(r, len));
+  int32_t* const row = r.tables + (size_t)b * r.max_pages;
+  const int32_t* const from = r.tables + (size_t)p * r.max_pages;
+  for (int j = threadIdx.x; j < r.max_pages; j += kRowThreads) {
+    if (j < had) count(r, row[j], -1);
+    const int32_t page = j < get ? from[j] : -1;
+    row[j] = page;
+    count(r, page, 1);
+  }
+  __syncthreads();  // all have read the row's own length
+  if (threadIdx.x == 0) lens[b] = len;
+}
+
+// ------------------------------------------------------------ resize
+
+struct Resize {
+  Rows rows;
+  const int32_t *lens, *new_lens;
+  int32_t *granted, *copies;
+  int32_t* offsets;  // [num_seqs] into fresh, -1: not granted
+  int32_t* copied;   // [num_seqs] whether the first of them replaces the last page
+  int32_t* fresh;    // [num_pages] the free pages that are handed out
+};
+
+__global__ __launch_bounds__(kRowThreads) void give_back_kernel(Resize a) {
+  const Rows& r = a.rows;
+  const int b = blockIdx.x;
+  const int had = pages_of(r, clipped(r, a.lens[b])), get = pages_of(r, clipped(r, a.new_lens[b]));
+  int32_t* const row = r.tables + (size_t)b * r.max_pages;
+  for (int j = get + threadIdx.x; j < had; j += kRowThreads) {
+    count(r, row[j], -1);
+    row[j] = -1;
+  }
+}
+
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanWaves = kPlanThreads / 64;
+
+// Sum of x over the threads before this one; *total over all.
+__device__ __forceinline__ int64_t scan(int64_t x, int64_t* lds, int64_t* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int64_t sum = x;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int64_t y = __shfl_up(sum, off);
+    if (lane >= off) sum += y;
+  }
+  __syncthreads();  // lds is free
+  if (lane == 63) lds[wave] = sum;
+  __syncthreads();
+  int64_t before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) {
+    before += w < wave ? lds[w] : 0;
+    all += lds[w];
+  }
+  *total = all;
+  return before + sum - x;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(Resize a) {
+  __shared__ int64_t lds_scan[kPlanWaves];
+  const Rows& r = a.rows;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // free pages before each wave's share of them, and in all
+  const int per = (int)(((int64_t)r.num_pages + kPlanThreads - 1) / kPlanThreads) * 64;  // pages of a wave
+  const int64_t first = (int64_t)wave * per;
+  int64_t mine = 0;
+  for (int i = 0; i < per; i += 64) {
+    const int64_t page = first + i + lane;
+    mine += __builtin_popcountll(__ballot(page < r.num_pages && r.refs[page] <= 0));
+  }
+  int64_t free_pages = 0;
+  int64_t before = scan(lane == 0 ? mine : 0, lds_scan, &free_pages);
+  before = __shfl(before, 0);
+
+  int64_t needed = 0;  // by the rows so far
+  for (int base = 0; base < r.num_seqs; base += kPlanThreads) {
+    const int b = base + tid;
+    int need = 0;
+    bool again = false, fits = false;
+    if (b < r.num_seqs) {
+      const int64_t len = clipped(r, a.lens[b]);
+      const int64_t want = a.new_lens[b] < 0 ? 0 : a.new_lens[b];
+      fits = want <= (int64_t)r.max_pages * r.page_tokens;
+      if (fits && want > len) {
+        const int had = pages_of(r, len);
+        if (len % r.page_tokens > 0) {
+          const int32_t last = r.tables[(size_t)b * r.max_pages + had - 1];
+          again = is_page(r, last) && r.refs[last] > 1;
+        }
+        need = pages_of(r, want) - had + (again ? 1 : 0);
+      }
+    }
+    int64_t all = 0;
+    const int64_t at = needed + scan(need, lds_scan, &all);
+    if (b < r.num_seqs) {
+      const bool ok = fits && (need == 0 || at + need <= free_pages);
+      a.offsets[b] = ok ? (int32_t)(need == 0 ? 0 : at) : -1;
+      a.copied[b] = ok && again ? 1 : 0;
+    }
+    needed += all;
+  }
+  // the lowest free pages, as many as may be handed out
+  const int64_t most = needed < free_pages ? needed : free_pages;
+  for (int i = 0; i < per && before < most; i += 64) {
+    const int64_t page = first + i + lane;
+    const unsigned long long who = __ballot(page < r.num_pages && r.refs[page] <= 0);
+    const int64_t at =
+        before + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u));
+    if ((who >> lane & 1) && at < most) a.fresh[at] = (int32_t)page;
+    before += __builtin_popcountll(who);
+  }
+}
+
+__global__ __launch_bounds__(kRowThreads) void grow_kernel(Resize a) {
+  const Rows& r = a.rows;
+  const int b = blockIdx.x;
+  const int64_t len = clipped(r, a.lens[b]);
+  const int64_t want = a.new_lens[b] < 0 ? 0 : a.new_lens[b];
+  const int at = a.offsets[b];
+  const int again = a.copied[b];
+  if (at >= 0 && want > len) {
+    const int had = pages_of(r, len), get = pages_of(r, want);
+    int32_t* const row = r.tables + (size_t)b * r.max_pages;
+    for (int j = had - again + (int)threadIdx.x; j < get; j += kRowThreads) {
+      const int32_t page = a.fresh[at + j - had + again];
+      if (j < had) {
+        const int32_t last = row[j];
+        count(r, last, -1);
+        reinterpret_cast<int2*>(a.copies)[b] = make_int2(last, page);
+      }
+      row[j] = page;
+      atomicExch(r.refs + page, 1);
+    }
+  }
+  __syncthreads();  // all have read the row's lengths
+  if (threadIdx.x == 0) {
+    a.granted[b] = at >= 0 ? (int32_t)want : (int32_t)len;
+    if (!again) reinterpret_cast<int2*>(a.copies)[b] = make_int2(-1, -1);
+  }
+}
+
+// ------------------------------------------------------------ copy
+
+constexpr int kCopyThreads = 256;
+constexpr int kCopyLoads = 8;  // 16 bytes each
+constexpr int kCopyChunk = kCopyThreads * kCopyLoads * 16;
+
+__global__ __launch_bounds__(kCopyThreads) void copy_kernel(uint16_t* k, uint16_t* v, const int32_t* __restrict__ copies,
+                                                            int32_t num_pages, int64_t page_bytes, int32_t parts) {
+  const int part = (int)blockIdx.x % parts;
+  const int pair = (int)blockIdx.x / parts;
+  const int2 c = reinterpret_cast<const int2*>(copies)[pair];
+  if (c.x < 0 || c.x >= num_pages || c.y < 0 || c.y >= num_pages || c.x == c.y) return;
+  char* const base = reinterpret_cast<char*>(blockIdx.y == 0 ? k : v);
+  const char* const src = base + (int64_t)c.x * page_bytes;
+  char* const dst = base + (int64_t)c.y * page_bytes;
+  u32x4 x[kCopyLoads];
+#pragma unroll
+  for (int i = 0; i < kCopyLoads; ++i) {
+    const int64_t at = (int64_t)part * kCopyChunk + (i * kCopyThreads + (int)threadIdx.x) * 16;
+    if (at < page_bytes) x[i] = *reinterpret_cast<const u32x4*>(src + at);
+  }
+#pragma unroll
+  for (int i = 0; i < kCopyLoads; ++i) {
+    const int64_t at = (int64_t)part * kCopyChunk + (i * kCopyThreads + (int)threadIdx.x) * 16;
+    if (at < page_bytes) *reinterpret_cast<u32x4*>(dst + at) = x[i];
+  }
+}
+
+// ------------------------------------------------------------ compact
+
+constexpr int kMoveThreads = 256;
+constexpr int kHeadLanes = 16;                                // 16 bytes each
+constexpr int kMoveRows = kMoveThreads / kHeadLanes;          // tokens per load of the workgroup
+constexpr int kMoveLoads = 8;
+constexpr int kMoveTokens = kMoveRows * kMoveLoads;           // of a block
+
+struct Compact {
+  uint16_t *k, *v;
+  const int32_t *tables, *lens, *q_starts, *q_lens, *keep, *keep_lens;
+  int32_t num_pages, max_pages, page_tokens, hkv, total_q;
+  int32_t* new_lens;
+};
+
+// One workgroup per (sequence, cache, head).
+__global__ __launch_bounds__(kMoveThreads) void compact_kernel(Compact a) {
+  __shared__ int32_t lds_from[2][kMoveTokens], lds_to[2][kMoveTokens];  // cache rows, -1: nothing to move
+  const int tid = threadIdx.x;
+  const int slices = 2 * a.hkv;
+  const int b = (int)blockIdx.x / slices;
+  const int slice = (int)blockIdx.x - b * slices;
+  const int len = a.lens[b] < 0 ? 0 : a.lens[b];
+  const int n = a.q_lens[b] < 0 ? 0 : a.q_lens[b] < len ? a.q_lens[b] : len;
+  const int kept = a.keep_lens[b] < 0 ? 0 : a.keep_lens[b] < n ? a.keep_lens[b] : n;
+  const int hist = len - n;
+  if (slice == 0 && tid == 0 && a.new_lens != nullptr) a.new_lens[b] = hist + kept;
+  const int64_t row0 = a.q_starts[b];
+  const int32_t* const table = a.tables + (size_t)b * a.max_pages;
+  uint16_t* const base = (slice < a.hkv ? a.k : a.v) + (size_t)(slice < a.hkv ? slice : slice - a.hkv) * kHeadDim;
+  auto row_of = [&](int t) {
+    const int j = t / a.page_tokens;
+    if (j >= a.max_pages) return -1;
+    const int page = table[j];
+    return page >= 0 && page < a.num_pages ? page * a.page_tokens + (t - j * a.page_tokens) : -1;
+  };
+  auto look_up = [&](int i0, int buf) {
+    if (tid < kMoveTokens) {
+      const int i = i0 + tid;
+      int from = -1, to = -1;
+      const int64_t row = row0 + i;
+      if (i < kept && row >= 0 && row < a.total_q) {
+        const int t = a.keep[row];
+        if (t >= 0 && t < n && t != i) {
+          from = row_of(hist + t);
+          to = row_of(hist + i);
+        }
+      }
+      lds_from[buf][tid] = to < 0 ? -1 : from;
+      lds_to[buf][tid] = to;
+    }
+  };
+  const int group = tid / kHeadLanes;
+  const int at = (tid % kHeadLanes) * 8;
+  const size_t row_elems = (size_t)a.hkv * kHeadDim;
+  look_up(0, 0);
+  __syncthreads();
+  for (int i0 = 0, buf = 0; i0 < kept; i0 += kMoveTokens, buf ^= 1) {
+    u32x4 x[kMoveLoads];
+#pragma unroll
+    for (int u = 0; u < kMoveLoads; ++u) {
+      const int from = lds_from[buf][u * kMoveRows + group];
+      x[u] = u32x4{0u, 0u, 0u, 0u};
+      if (from >= 0) x[u] = *reinterpret_cast<const u32x4*>(base + from * row_elems + at);
+    }
+    look_up(i0 + kMoveTokens, buf ^ 1);
+    // every thread's loads have arrived before any store
+#pragma unroll
+    for (int u = 0; u < kMoveLoads; ++u) asm volatile("" : "+v"(x[u]));
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kMoveLoads; ++u) {
+      const int i = u * kMoveRows + group;
+      if (lds_from[buf][i] >= 0) *reinterpret_cast<u32x4*>(base + lds_to[buf][i] * row_elems + at) = x[u];
+    }
+    __syncthreads();  // the lists may be written again
+  }
+}
+
+int check_rows(ctx_decode_attn* h, int32_t num_seqs, int32_t max_pages, int32_t num_pages) {
+  int rc = check_common(h, num_seqs, 1.0f);
+  if (rc != CTX_OK) return rc;
+  if (h->desc.page_tokens <= 0) return fail(CTX_ERR_UNSUPPORTED, "the handle was created without page_tokens");
+  if (num_pages < 0 || max_pages <= 0)
+    return fail(CTX_ERR_INVALID_ARG, "num_pages must not be negative and max_pages_per_seq must be positive");
+  if ((int64_t)num_pages * h->desc.page_tokens > kMostTokens)
+    return fail(CTX_ERR_UNSUPPORTED, "caches of more than %d tokens", kMostTokens);
+  return CTX_OK;
+}
+
+Rows rows_of(const ctx_decode_attn* h, int32_t* tables, int32_t max_pages, int32_t num_seqs, int32_t* refs,
+             int32_t num_pages) {
+  return Rows{tables, max_pages, h->desc.page_tokens, num_seqs, refs, num_pages};
+}
+
+int launched() {
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? CTX_OK : hip_fail(e, "kernel launch");
+}
+
+}  // namespace
+
+extern "C" int ctx_kv_fork_run_paged(ctx_decode_attn* h, int32_t* block_tables, int32_t max_pages_per_seq,
+                                     int32_t* seq_lens, int32_t num_seqs, const int32_t* parents, int32_t* page_refs,
+                                     int32_t num_pages, void* stream) {
+  int rc = check_rows(h, num_seqs, max_pages_per_seq, num_pages);
+  if (rc != CTX_OK) return rc;
+  if (num_seqs == 0) return CTX_OK;
+  if (block_tables == nullptr || seq_lens == nullptr || parents == nullptr ||
+      (page_refs == nullptr && num_pages > 0))
+    return fail(CTX_ERR_INVALID_ARG, "NULL data pointer");
+  if ((rc = check_device(h)) != CTX_OK) return rc;
+  hipLaunchKernelGGL(fork_kernel, dim3((unsigned)num_seqs), dim3(kRowThreads), 0, reinterpret_cast<hipStream_t>(stream),
+                     rows_of(h, block_tables, max_pages_per_seq, num_seqs, page_refs, num_pages), seq_lens, parents);
+  return launched();
+}
+
+extern "C" size_t ctx_kv_resize_workspace(int32_t num_seqs, int32_t num_pages) {
+  const size_t seqs = num_seqs > 0 ? (size_t)num_seqs : 0, pages = num_pages > 0 ? (size_t)num_pages : 0;
+  return (2 * seqs + pages) * sizeof(int32_t);
+}
+
+extern "C" int ctx_kv_resize_run_paged(ctx_decode_attn* h, int32_t* block_tables, int32_t max_pages_per_seq,
+                                       const int32_t* seq_lens, const int32_t* new_lens, int32_t num_seqs,
+                                       int32_t* page_refs, int32_t num_pages, int32_t* granted, int32_t* copies,
+                                       void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_rows(h, num_seqs, max_pages_per_seq, num_pages);
+  if (rc != CTX_OK) return rc;
+  if (num_seqs == 0) return CTX_OK;
+  if (block_tables == nullptr || seq_lens == nullptr || new_lens == nullptr || (page_refs == nullptr && num_pages > 0) ||
+      granted == nullptr || copies == nullptr || workspace == nullptr)
+    return fail(CTX_ERR_INVALID_ARG, "NULL data pointer");
+  if (!aligned16(workspace) || (reinterpret_cast<uintptr_t>(copies) & 7u) != 0)
+    return fail(CTX_ERR_ALIGNMENT, "workspace must be 16-byte and copies 8-byte aligned");
+  const size_t need = ctx_kv_resize_workspace(num_seqs, num_pages);
+  if (workspace_bytes < need) return fail(CTX_ERR_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+  if ((rc = check_device(h)) != CTX_OK) return rc;
+  Resize a{};
+  a.rows = rows_of(h, block_tables, max_pages_per_seq, num_seqs, page_refs, num_pages);
+  a.lens = seq_lens;
+  a.new_lens = new_lens;
+  a.granted = granted;
+  a.copies = copies;
+  a.offsets = static_cast<int32_t*>(workspace);
+  a.copied = a.offsets + num_seqs;
+  a.fresh = a.copied + num_seqs;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  hipLaunchKernelGGL(give_back_kernel, dim3((unsigned)num_seqs), dim3(kRowThreads), 0, s, a);
+  hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
+  hipLaunchKernelGGL(grow_kernel, dim3((unsigned)num_seqs), dim3(kRowThreads), 0, s, a);
+  return launched();
+}
+
+extern "C" int ctx_kv_copy_run_paged(ctx_decode_attn* h, void* k_pages, void* v_pages, int32_t num_pages,
+                                     const int32_t* copies, int32_t num_copies, void* stream) {
+  int rc = check_rows(h, 0, 1, num_pages);
+  if (rc != CTX_OK) return rc;
+  if (num_copies < 0) return fail(CTX_ERR_INVALID_ARG, "num_copies %d < 0", num_copies);
+  if (num_copies == 0 || num_pages == 0) return CTX_OK;
+  if (k_pages == nullptr || v_pages == nullptr || copies == nullptr) return fail(CTX_ERR_INVALID_ARG, "NULL data pointer");
+  if (!aligned16(k_pages) || !aligned16(v_pages) || (reinterpret_cast<uintptr_t>(copies) & 7u) != 0)
+    return fail(CTX_ERR_ALIGNMENT, "k_pages and v_pages must be 16-byte and copies 8-byte aligned");
+  if ((rc = check_device(h)) != CTX_OK) return rc;
+  const int64_t page_bytes = (int64_t)h->desc.page_tokens * h->desc.num_kv_heads * kHeadDim * 2;
+  const int64_t parts = (page_bytes + kCopyChunk - 1) / kCopyChunk;
+  if (parts * num_copies > kMostTokens) return fail(CTX_ERR_INVALID_ARG, "copy grid too large");
+  hipLaunchKernelGGL(copy_kernel, dim3((unsigned)(parts * num_copies), 2), dim3(kCopyThreads), 0,
+                     reinterpret_cast<hipStream_t>(stream), static_cast<uint16_t*>(k_pages),
+                     static_cast<uint16_t*>(v_pages), copies, num_pages, page_bytes, (int32_t)parts);
+  return launched();
+}
+
+extern "C" int ctx_kv_compact_run_paged(ctx_decode_attn* h, void* k_pages, void* v_pages, int32_t num_pages,
+                                        const int32_t* block_tables, int32_t max_pages_per_seq,
+                                        const int32_t* seq_lens, const int32_t* q_starts, const int32_t* q_lens,
+                                        const int32_t* keep, const int32_t* keep_lens, int32_t num_seqs,
+                                        int32_t total_q, int32_t* new_lens, void* stream) {
+  int rc = check_rows(h, num_seqs, max_pages_per_seq, num_pages);
+  if (rc != CTX_OK) return rc;
+  if (total_q < 0) return fail(CTX_ERR_INVALID_ARG, "total_q %d < 0", total_q);
+  if (num_seqs == 0) return CTX_OK;
+  if (k_pages == nullptr || v_pages == nullptr || block_tables == nullptr || seq_lens == nullptr || q_starts == nullptr ||
+      q_lens == nullptr || keep_lens == nullptr || (keep == nullptr && total_q > 0))
+    return fail(CTX_ERR_INVALID_ARG, "NULL data pointer");
+  if (new_lens != nullptr && (new_lens == seq_lens || new_lens == q_lens || new_lens == keep_lens || new_lens == q_starts))
+    return fail(CTX_ERR_INVALID_ARG, "new_lens may not be an input");
+  if (!aligned16(k_pages) || !aligned16(v_pages))
+    return fail(CTX_ERR_ALIGNMENT, "k_pages and v_pages must be 16-byte aligned");
+  if ((rc = check_device(h)) != CTX_OK) return rc;
+  Compact a{};
+  a.k = static_cast<uint16_t*>(k_pages);
+  a.v = static_cast<uint16_t*>(v_pages);
+  a.tables = block_tables;
+  a.lens = seq_lens;
+  a.q_starts = q_starts;
+  a.q_lens = q_lens;
+  a.keep = keep;
+  a.keep_lens = keep_lens;
+  a.num_pages = num_pages;
+  a.max_pages = max_pages_per_seq;
+  a.page_tokens = h->desc.page_tokens;
+  a.hkv = h->desc.num_kv_heads;
+  a.total_q = total_q;
+  a.new_lens = new_lens;
+  const int64_t grid = (int64_t)num_seqs * 2 * a.hkv;
+  if (grid > kMostTokens) return fail(CTX_ERR_INVALID_ARG, "compaction grid too large");
+  hipLaunchKernelGGL(compact_kernel, dim3((unsigned)grid), dim3(kMoveThreads), 0, reinterpret_cast<hipStream_t>(stream), a);
+  return launched();
+}
