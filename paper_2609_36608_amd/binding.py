@@ -44,6 +44,8 @@ EXPORTS = (
     "ctx_kv_append_run_paged",
     "ctx_prefill_attn_run_paged",
     "ctx_decode_attn_run_paged_scored",
+    "ctx_tree_attn_workspace",
+    "ctx_tree_attn_run_paged",
     "ctx_kv_fork_run_paged",
     "ctx_kv_resize_workspace",
     "ctx_kv_resize_run_paged",
@@ -167,6 +169,11 @@ def load_library(path: str | None = None):
                                      ctypes.POINTER(OpdParams), vp, vp, vp, vp, vp, ctypes.c_int64, vp]
     lib.ctx_opd_loss_run.restype = ctypes.c_int
     size_t, i64, f32 = ctypes.c_size_t, ctypes.c_int64, ctypes.c_float
+    lib.ctx_tree_attn_workspace.argtypes = [vp, i32, i32, ctypes.POINTER(size_t)]
+    lib.ctx_tree_attn_workspace.restype = ctypes.c_int
+    lib.ctx_tree_attn_run_paged.argtypes = [vp, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, i32, i32, i32, f32,
+                                            ctypes.POINTER(CtxAttnScores), vp, vp, size_t, vp]
+    lib.ctx_tree_attn_run_paged.restype = ctypes.c_int
     lib.ctx_kv_fork_run_paged.argtypes = [vp, vp, i32, vp, i32, vp, vp, i32, vp]
     lib.ctx_kv_fork_run_paged.restype = ctypes.c_int
     lib.ctx_kv_resize_workspace.argtypes = [i32, i32]
@@ -535,6 +542,54 @@ class DecodeAttention:
         if rc != CTX_OK:
             raise error_for(self.lib, rc)
         return out
+
+    def tree_paged(self, q, k_pages, v_pages, block_tables, seq_lens, q_starts, q_lens, parents, max_q_len: int,
+                   scale: float, out, scores: AttnScores | None = None, workspace=None, stream=None):
+        """Attention of drafted trees over paged caches (ctx_tree_attn_run_paged): q / out [rows, Hq, D];
+        sequence b's q_lens[b] drafts (rows q_starts[b] ..) are the last of its seq_lens[b] tokens, whose
+        keys and values are in the pages.  parents int32 [rows]: -1, or the index of a draft's parent
+        among its sequence's drafts before it (any other value: a padding row).  A draft sees the tokens
+        before the drafts, its ancestors and itself; scores (without doc_starts) changes scores and
+        masks by positions, which count depths.  workspace: uint8, at least tree_workspace bytes; None:
+        allocated on the stream that the call runs on.  Calls that may overlap need one each."""
+        import torch
+
+        if self.handle is None:
+            raise RuntimeError("handle is closed")
+        dev, b, rows = self.device, seq_lens.shape[0], q.shape[0]
+        _need("q", q, torch.bfloat16, dev, (rows, self.q_heads, HEAD_DIM))
+        _need("out", out, self.out_dtype, dev, (rows, self.q_heads, HEAD_DIM))
+        for name, t in (("seq_lens", seq_lens), ("q_starts", q_starts), ("q_lens", q_lens)):
+            _need(name, t, torch.int32, dev, (b,))
+        _need("parents", parents, torch.int32, dev, (rows,))
+        self._check_pages(k_pages, v_pages, block_tables, b)
+        if scores is not None and scores.doc_starts is not None:
+            raise ValueError("trees have no doc_starts")
+        max_q_len = _int32("max_q_len", max_q_len)
+        if workspace is None:
+            size = self.tree_workspace(b, max_q_len)
+            with _allocating_on(stream, q.device):
+                workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+        else:
+            _need("workspace", workspace, torch.uint8, dev, (workspace.numel(),))
+        rc = self.lib.ctx_tree_attn_run_paged(
+            self.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), k_pages.shape[0], block_tables.data_ptr(),
+            block_tables.shape[1], seq_lens.data_ptr(), q_starts.data_ptr(), q_lens.data_ptr(), parents.data_ptr(), b, rows,
+            max_q_len, scale, _scores_struct(scores, dev, self.q_heads, b, rows), out.data_ptr(), workspace.data_ptr(),
+            workspace.numel(), self._stream(stream))
+        if rc != CTX_OK:
+            raise error_for(self.lib, rc)
+        return out
+
+    def tree_workspace(self, num_seqs: int, max_q_len: int) -> int:
+        """Bytes of workspace of a tree_paged call (ctx_tree_attn_workspace)."""
+        if self.handle is None:
+            raise RuntimeError("handle is closed")
+        size = ctypes.c_size_t()
+        rc = self.lib.ctx_tree_attn_workspace(self.handle, num_seqs, max_q_len, ctypes.byref(size))
+        if rc != CTX_OK:
+            raise error_for(self.lib, rc)
+        return size.value
 
     def _check_rows(self, block_tables, seq_lens, page_refs) -> int:
         """Rows of a block table whose pages are counted."""

@@ -11,11 +11,9 @@ from concurrent.futures import ThreadPoolExecutor
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "ctx_decode_attn.hip")
-SRCS = [SRC, os.path.join(PKG, "csrc", "ctx_prefill_attn.hip"), os.path.join(PKG, "csrc", "ctx_prefill_paged.hip"),
-        os.path.join(PKG, "csrc", "ctx_kv_append.hip"), os.path.join(PKG, "csrc", "ctx_kv_pages.hip"),
-        os.path.join(PKG, "csrc", "ctx_opd_loss.hip"),
-        os.path.join(PKG, "csrc", "ctx_token_logprob.hip"),
-        os.path.join(PKG, "csrc", "ctx_ceiling_probe.hip"), os.path.join(PKG, "csrc", "ctx_rollout_sim.cpp")]
+SRCS = [SRC, *(os.path.join(PKG, "csrc", name) for name in (
+    "ctx_prefill_attn.hip", "ctx_prefill_paged.hip", "ctx_tree_attn.hip", "ctx_kv_append.hip", "ctx_kv_pages.hip",
+    "ctx_opd_loss.hip", "ctx_token_logprob.hip", "ctx_ceiling_probe.hip", "ctx_rollout_sim.cpp"))]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libctx_decode_attn.so")
 ARCH = "gfx950"

@@ -55,13 +55,13 @@
 
 #include "ctx_attn_common.h"
 #include "ctx_paged_attn.h"
+#include "ctx_paged_common.h"
 
 namespace {
 
 // the query tiles of one (sequence, KV head) re-read the same blocks, mostly from L2
 constexpr int kLoadPolicy = 0;
 
-typedef __attribute__((address_space(3))) void lds_void;
 constexpr int kWideWaves = 4;
 constexpr int wg_waves(int split) { return split > 0 ? split : kWideWaves; }
 constexpr int kBlock = 32;  // tokens
@@ -82,25 +82,6 @@ enum Change { kPlain, kBias, kCap, kCapBias };
 // cap of 512), 1,024 over 4,000 169 (134).  One-term kernels with that cap, in wide
 // workgroups of one tile alone, took 479 and 155 us.
 constexpr float kFarFrom = 512.f;
-
-// s_waitcnt vmcnt(n) with expcnt and lgkmcnt left open
-constexpr int wait_vmcnt(int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); }
-
-// Quotients of 0 <= x < 2^31 by d > 0, exact: with 2^(shift - 1) < d <= 2^shift the factor's
-// excess over 2^(31 + shift) / d is less than 1, which x / 2^31 of cannot carry the
-// quotient over the next whole number.  (Three instructions where a division takes 30, and
-// a workgroup has a dozen before its first block.)
-struct Divisor {
-  int32_t d;
-  uint32_t factor;
-  int32_t shift;
-  Divisor() = default;
-  explicit Divisor(int32_t by) : d(by), shift(0) {
-    while (((int64_t)1 << shift) < by) ++shift;
-    factor = (uint32_t)((((uint64_t)1 << (31 + shift)) + by - 1) / by);
-  }
-  __device__ __forceinline__ int of(int x) const { return (int)(__umulhi((uint32_t)x << 1, factor) >> shift); }
-};
 
 struct PagedPlan {
   const int32_t *block_tables, *lens, *q_starts, *q_lens;
@@ -123,31 +104,6 @@ struct PagedPlan {
   float factor;        // of the product in log2 units, without a cap
   float cap_in, cap_in2, cap_out;  // scale / cap, twice that and cap in log2 units
 };
-
-// Workgroup barrier with no memory fence: the caller has already waited for its own
-// loads into LDS that the other waves will read, and a fence would also wait for the
-// loads of later blocks still in flight.
-__device__ __forceinline__ void lds_barrier() { asm volatile("s_barrier" ::: "memory"); }
-
-// 16 bytes per lane from voff in r straight to LDS base + 16 * lane
-__device__ __forceinline__ void load16_to_lds(__amdgpu_buffer_rsrc_t r, uint16_t* base, int voff) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)base, 16, voff, 0, 0, kLoadPolicy);
-}
-
-// NaN-propagating maximum of 8, which gfx950 has as a three-input instruction
-__device__ __forceinline__ float max8(f32x4 a, f32x4 b) {
-  const auto mx = [](float x, float y) { return __builtin_elementwise_maximum(x, y); };
-  return mx(mx(mx(mx(a[0], a[1]), a[2]), mx(mx(a[3], b[0]), b[1])), mx(b[2], b[3]));
-}
-
-// the largest of a column, whose tokens are spread over the 4 rows of 16 lanes
-__device__ __forceinline__ float column_max(float x) {
-  const uint32_t a = __float_as_uint(x);
-  const auto rows = __builtin_amdgcn_permlane16_swap(a, a, false, false);
-  const uint32_t b = __float_as_uint(fmaxf(__uint_as_float(rows[0]), __uint_as_float(rows[1])));
-  const auto halves = __builtin_amdgcn_permlane32_swap(b, b, false, false);
-  return fmaxf(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
-}
 
 // the least or largest over a row of 16 lanes, by rotations; the rows of a wave hold the
 // same columns
@@ -467,7 +423,7 @@ __global__ __launch_bounds__(64 * wg_waves(kSplit)) __attribute__((amdgpu_waves_
           make_rsrc(reinterpret_cast<const uint16_t*>(from), (w.h[h] & 31) * (uint32_t)row_bytes);
 #pragma unroll
       for (int r = 0; r < kRounds; ++r)
-        load16_to_lds(rs, dst + h * kHalf * kHeadDim + (r * kStagers + stage_wave) * 4 * kHeadDim, off[h][r]);
+        load16_to_lds<kLoadPolicy>(rs, dst + h * kHalf * kHeadDim + (r * kStagers + stage_wave) * 4 * kHeadDim, off[h][r]);
     }
   };
 
