@@ -11,8 +11,11 @@
 //     one per workgroup; a workgroup finds its own from the lengths.  An item that lies
 //     within a range gets its outputs at once; of the others each workgroup writes a partial
 //     one, at most two, and tree_join_kernel joins them in order.
-//   * A workgroup's waves share every block through a three-stage LDS tile, loaded
-//     two blocks ahead, each wave with columns of its own; waves without columns only load.
+//   * A workgroup has 8 waves on a CU of its own.  With up to 128 columns four waves hold the
+//     columns and the two fours take one of two neighbouring blocks each, joined
+//     through LDS at the item's end; with more, all eight hold columns.  The blocks
+//     pass through four stages of LDS tiles, loaded three steps ahead by all waves; waves
+//     without columns only load.
 //   * Trees: the ancestors of every draft, as a mask of bits, by doubling: with the ancestors up
 //     to 2^k steps up known, those up to 2^(k+1) are these and those of the one 2^k up.
 //     They are needed for the blocks that hold drafts, and elsewhere only for the drafts'
@@ -110,35 +113,43 @@ __device__ __forceinline__ int64_t quota_of(int64_t total, int ranges) {
   return even > kLeastBlocks ? even : kLeastBlocks;
 }
 
-template <int kWaves, int kTiles>
-constexpr int kColsOf = kWaves* kTiles * 16;
+constexpr int kWaves = 8;
+constexpr int kStages = 4;  // of a step's blocks in LDS
+
+// Column waves (the others take other blocks) and 16-column tiles per wave.
+template <int kColWaves, int kTiles>
+constexpr int kColsOf = kColWaves* kTiles * 16;
 
 // kTerms: bf16 terms of each softmax weight, 1, 2 (16 bits) or 3 (24).
-template <typename OutT, int kTerms, int kChange, int kWaves, int kTiles>
+template <typename OutT, int kTerms, int kChange, int kColWaves, int kTiles>
 __global__ __launch_bounds__(64 * kWaves) void tree_attn_kernel(const uint16_t* __restrict__ q,
                                                                 const uint16_t* __restrict__ kc,
                                                                 const uint16_t* __restrict__ vc, TreePlan pp,
                                                                 OutT* __restrict__ out) {
   constexpr bool kHasBias = (kChange & 1) != 0;
   constexpr bool kHasCap = kChange >= kCap;
-  constexpr int kCols = kColsOf<kWaves, kTiles>;
+  constexpr int kCols = kColsOf<kColWaves, kTiles>;
   constexpr int kNodes = kCols < kMostDrafts ? kCols : kMostDrafts;  // most drafts of a sequence
   constexpr int kWords = kNodes / 32;
-  constexpr int kRounds = kBlock / (4 * kWaves);  // loads per thread and block of K, and of V
-  constexpr int kLoads = 2 * kRounds;
-  static_assert(kWaves == 4 || kWaves == 8, "a wave loads four tokens of a half block");
+  constexpr int kStep = kWaves / kColWaves;  // blocks of a step; also loads per thread of its K, and of its V
+  constexpr int kLoads = 2 * kStep;
+  constexpr int kStageElems = kStep * kBlockElems;
+  static_assert(kWaves * 4 == kBlock, "a wave loads four tokens of every block");
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col_wave = wave % kColWaves;
+  const int part_wave = wave / kColWaves;  // which block of a step
   const int n = lane & 15;
   const int c = lane >> 4;
   const int g = pp.group.d;
 
-  // three stages, distinct arrays named at compile time, so that the compiler's waits before the
-  // reads cover only their own stage's loads
-  __shared__ __attribute__((aligned(16))) uint16_t lds_k0[kBlockElems], lds_v0[kBlockElems];
-  __shared__ __attribute__((aligned(16))) uint16_t lds_k1[kBlockElems], lds_v1[kBlockElems];
-  __shared__ __attribute__((aligned(16))) uint16_t lds_k2[kBlockElems], lds_v2[kBlockElems];
+  // stages of K and V, distinct arrays named at compile time, so that the compiler's waits before
+  // the reads cover only their own stage's loads
+  __shared__ __attribute__((aligned(16))) uint16_t lds_k0[kStageElems], lds_v0[kStageElems];
+  __shared__ __attribute__((aligned(16))) uint16_t lds_k1[kStageElems], lds_v1[kStageElems];
+  __shared__ __attribute__((aligned(16))) uint16_t lds_k2[kStageElems], lds_v2[kStageElems];
+  __shared__ __attribute__((aligned(16))) uint16_t lds_k3[kStageElems], lds_v3[kStageElems];
   __shared__ uint32_t lds_mask[kNodes][kWords];  // bit a of draft i: it sees draft a
   __shared__ int16_t lds_depth[kNodes];          // -1: padding
   __shared__ int16_t lds_up[kNodes];
@@ -208,7 +219,7 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kernel(const uint16_t* 
   // of a half block, and each lane fetches the chunk that the swizzle puts at its slot.
   const int load_tok = (wave & 3) * 4 + (lane >> 4);  // within the half
   const int load_off = load_tok * row_bytes + (((lane & 15) ^ tile_swizzle(load_tok)) << 4);
-  auto load_half = [&](int r) { return kWaves == 8 ? wave >> 2 : r; };
+  const int load_half = wave >> 2;
 
   int tree_of = -1;  // the sequence whose tree is in LDS
   for (; from < to; ++b) {
@@ -283,7 +294,7 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kernel(const uint16_t* 
 
       // this lane's columns
       auto row_at = [&](int ct) -> int64_t {  // first element of its query (and output) row, -1 without one
-        const int col = tile * kCols + (ct * kWaves + wave) * 16 + n;
+        const int col = tile * kCols + (ct * kColWaves + col_wave) * 16 + n;
         const int qi = pp.group.of(col);
         const int64_t row = (int64_t)row0 + qi;
         return qi < s.drafts && row >= 0 && row < pp.total_q ? (row * pp.hq + kv * g + (col - qi * g)) * kHeadDim : -1;
@@ -296,7 +307,7 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kernel(const uint16_t* 
       int all_low = 0;  // what every column of the wave sees past the prefix
 #pragma unroll
       for (int ct = 0; ct < kTiles; ++ct) {
-        const int col = tile * kCols + (ct * kWaves + wave) * 16 + n;
+        const int col = tile * kCols + (ct * kColWaves + col_wave) * 16 + n;
         const int qi = pp.group.of(col);
         const int64_t row = row_at(ct);
         draft[ct] = -1;
@@ -330,7 +341,7 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kernel(const uint16_t* 
         all_low = other > all_low ? other : all_low;
       }
       all_low = __builtin_amdgcn_readfirstlane(all_low);
-      const bool busy = pp.group.of(tile * kCols + wave * 16) < s.drafts;  // wave-uniform
+      const bool busy = pp.group.of(tile * kCols + col_wave * 16) < s.drafts;  // wave-uniform
 
       Softmax st[kTiles];
       int unset = (1 << kTiles) - 1;  // bit ct: the column has seen no token yet
@@ -371,21 +382,21 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kernel(const uint16_t* 
           }
         }
       };
-      auto word_at = [&](int u, int half) __attribute__((always_inline)) {
-        return (uint32_t)__builtin_amdgcn_readlane((int)halves, (u - held) * 2 + half);
-      };
-      int absent = 0;  // bits 2 j, 2 j + 1: a half of the block j steps on that is on no page
+      uint32_t absent = 0;  // a byte per step, the next one's lowest: bit h where half h is on no page
+      // the loads of the blocks u .. u + kStep - 1 into a stage
       auto issue = [&](int u, uint16_t* dk, uint16_t* dv, int ahead) __attribute__((always_inline)) {
         if (u - held >= kHeld / 2) look_up(u);
-        const uint32_t w0 = word_at(u, 0), w1 = word_at(u, 1);
-        absent |= (((w0 & 31) == 0 ? 1 : 0) | ((w1 & 31) == 0 ? 2 : 0)) << (2 * ahead);
 #pragma unroll
-        for (int r = 0; r < kRounds; ++r) {
-          const int h = load_half(r);
-          const uint32_t w = h == 0 ? w0 : w1;
+        for (int r = 0; r < kStep; ++r) {
+          const int lane0 = (u - held + r) * 2;
+          const uint32_t w0 = (uint32_t)__builtin_amdgcn_readlane((int)halves, lane0);
+          const uint32_t w1 = (uint32_t)__builtin_amdgcn_readlane((int)halves, lane0 + 1);
+          const uint32_t gone = ((w0 & 31) == 0 ? 1u : 0u) | ((w1 & 31) == 0 ? 2u : 0u);
+          if (r == part_wave) absent |= gone << (8 * ahead);
+          const uint32_t w = load_half == 0 ? w0 : w1;
           const uint64_t first = (uint64_t)(w >> 6) * (uint32_t)(kHalf * row_bytes);
           const uint32_t bytes = (w & 31) * (uint32_t)row_bytes;
-          const int to_lds = (h * kHalf + (wave & 3) * 4) * kHeadDim;
+          const int to_lds = r * kBlockElems + (load_half * kHalf + (wave & 3) * 4) * kHeadDim;
           int off = load_off;
           load16_to_lds<kLoadAux>(
               make_rsrc(reinterpret_cast<const uint16_t*>(reinterpret_cast<const char*>(khead) + first), bytes),
@@ -393,7 +404,7 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kernel(const uint16_t* 
           if (w & kEdge) {  // values that no draft sees may hold anything: zeros
             int at_tok = load_tok;
             asm volatile("" : "+v"(at_tok));
-            const int t = token(u * kBlock + h * kHalf) + at_tok;
+            const int t = token((u + r) * kBlock + load_half * kHalf) + at_tok;
             const bool hidden = t < s.hist ? t >= s.prefix && t < s.low : t < s.end && lds_depth[t - s.hist] < 0;
             if (hidden) off = kNowhere;
           }
@@ -584,38 +595,81 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kernel(const uint16_t* 
       // The queries have arrived with the table's entries; said here, the compiler need not
       // wait for them in the loop, where that would be a wait for the blocks in flight too.
       __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
-      // One block: wait for this wave's loads of it, then the barrier (every wave's have landed, and
+      // One step: wait for this wave's loads of it, then the barrier (every wave's have landed, and
       // every wave is done with the stage read in the previous step); the loads of the
-      // block two ahead go into that stage.
+      // step three ahead go into that stage.
       auto step = [&](int u, const uint16_t* kt, const uint16_t* vt, uint16_t* nk, uint16_t* nv)
           __attribute__((always_inline)) {
-        __builtin_amdgcn_s_waitcnt(wait_vmcnt(kLoads));
+        __builtin_amdgcn_s_waitcnt(wait_vmcnt((kStages - 2) * kLoads));
         lds_barrier();
         const int gone = absent & 3;
-        absent >>= 2;
-        issue(u + 2, nk, nv, 1);
-        if (u < last_block && busy) {
+        absent >>= 8;
+        issue(u + (kStages - 1) * kStep, nk, nv, kStages - 2);
+        const int mine = u + part_wave;
+        if (mine < last_block && busy) {
           f32x4 sc[kTiles][2];
           u32x4 pt[kTerms][kTiles];
-          scores(kt, sc);
-          relative(u, gone, sc);
+          scores(kt + part_wave * kBlockElems, sc);
+          relative(mine, gone, sc);
           raise(sc);
           weights(sc, pt);
-          values(vt, pt);
+          values(vt + part_wave * kBlockElems, pt);
         }
       };
       issue(first_block, lds_k0, lds_v0, 0);
-      issue(first_block + 1, lds_k1, lds_v1, 1);
-      // whole rounds of three steps; the last of them may be on empty blocks
-      for (int u = first_block; u < last_block; u += 3) {
-        step(u, lds_k0, lds_v0, lds_k2, lds_v2);
-        step(u + 1, lds_k1, lds_v1, lds_k0, lds_v0);
-        step(u + 2, lds_k2, lds_v2, lds_k1, lds_v1);
+      issue(first_block + kStep, lds_k1, lds_v1, 1);
+      issue(first_block + 2 * kStep, lds_k2, lds_v2, 2);
+      // whole rounds of four steps; the last of them may be on empty blocks
+      for (int u = first_block; u < last_block; u += kStages * kStep) {
+        step(u, lds_k0, lds_v0, lds_k3, lds_v3);
+        step(u + kStep, lds_k1, lds_v1, lds_k0, lds_v0);
+        step(u + 2 * kStep, lds_k2, lds_v2, lds_k1, lds_v1);
+        step(u + 3 * kStep, lds_k3, lds_v3, lds_k2, lds_v2);
       }
       // no load may land in a stage after the workgroup has gone on
       __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));
       __syncthreads();
 
+      if constexpr (kStep == 2) {
+        // the second four waves' sums and outputs go to the first four's, lane by lane, which scale
+        // both to the larger maximum
+        static_assert(kStageElems * 2 == 2 * 8 * 64 * 16 && kTiles <= 2, "a column wave's outputs fit a stage's keys");
+        float* const their_o = reinterpret_cast<float*>(col_wave == 0   ? lds_k0
+                                                        : col_wave == 1 ? lds_k1
+                                                        : col_wave == 2 ? lds_k2
+                                                                        : lds_k3);
+        float2* const their_ml = reinterpret_cast<float2*>(lds_v0) + col_wave * kTiles * 64;
+        if (part_wave == 1) {
+#pragma unroll
+          for (int ct = 0; ct < kTiles; ++ct) {
+            their_ml[ct * 64 + lane] = make_float2((unset >> ct & 1) ? -INFINITY : st[ct].m, st[ct].l);
+#pragma unroll
+            for (int nb = 0; nb < 8; ++nb)
+              *reinterpret_cast<f32x4*>(their_o + ((ct * 8 + nb) * 64 + lane) * 4) = o[ct][nb];
+          }
+        }
+        __syncthreads();
+        if (part_wave == 0) {
+#pragma unroll
+          for (int ct = 0; ct < kTiles; ++ct) {
+            const float2 ml = their_ml[ct * 64 + lane];
+            const float m0 = (unset >> ct & 1) ? -INFINITY : st[ct].m;
+            const float top = fmaxf(m0, ml.x);
+            const float a0 = m0 > -INFINITY ? fast_exp2(m0 - top) : 0.f;
+            const float a1 = ml.x > -INFINITY ? fast_exp2(ml.x - top) : 0.f;
+            if (top > -INFINITY) {
+              st[ct].m = top;
+              unset &= ~(1 << ct);
+            }
+            st[ct].l = a0 * st[ct].l + a1 * ml.y;
+#pragma unroll
+            for (int nb = 0; nb < 8; ++nb)
+              o[ct][nb] = a0 * o[ct][nb] + a1 * *reinterpret_cast<const f32x4*>(their_o + ((ct * 8 + nb) * 64 + lane) * 4);
+          }
+        }
+        __syncthreads();
+        if (part_wave != 0) continue;
+      }
 #pragma unroll
       for (int ct = 0; ct < kTiles; ++ct) {
         float l_tot = st[ct].l + __shfl_xor(st[ct].l, 16);
@@ -630,7 +684,7 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kernel(const uint16_t* 
           for (int nb = 0; nb < 8; ++nb)
             store4<OutT>(orow + 16 * nb, none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[ct][nb] * inv);
         } else {
-          const int64_t part = slot * kCols + (ct * kWaves + wave) * 16 + n;
+          const int64_t part = slot * kCols + (ct * kColWaves + col_wave) * 16 + n;
           if (c == 0) pp.ml_ws[part] = make_float2(padding[ct] ? INFINITY : none ? -INFINITY : st[ct].m, none ? 0.f : l_tot);
           float* orow = pp.o_ws + part * kHeadDim + 4 * c;
 #pragma unroll
@@ -642,73 +696,63 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kernel(const uint16_t* 
   }
 }
 
-// Joins the partial outputs of an item: one wave per (draft, head), two dimensions per lane, in the
-// order of ranges.
-constexpr int kJoinWaves = 4;
+// Joins the partial outputs of the items: a workgroup per 16-column tile of an item, 32 lanes of
+// 4 dimensions per column, in the order of ranges.
+constexpr int kJoinThreads = 256;
+constexpr int kJoinCols = 16;
 
 template <typename OutT, int kCols>
-__global__ __launch_bounds__(64 * kJoinWaves) void tree_join_kernel(TreePlan pp, OutT* __restrict__ out) {
-  const int lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * kJoinWaves + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  const int64_t draft_id = id / pp.hq;
-  const int head = (int)(id - draft_id * pp.hq);
-  const int b = (int)(draft_id / pp.max_q_len);
-  const int i = (int)(draft_id - (int64_t)b * pp.max_q_len);
-  if (b >= pp.num_seqs) return;
+__global__ __launch_bounds__(kJoinThreads) void tree_join_kernel(TreePlan pp, int tiles16, OutT* __restrict__ out) {
+  const int t16 = (int)blockIdx.x % tiles16;
+  const int unit = (int)blockIdx.x / tiles16;
+  const int b = unit / pp.hkv, kv = unit - b * pp.hkv;
   const Seen s = seen_of(pp, b);
-  const int64_t row = (int64_t)pp.q_starts[b] + i;
-  if (i >= s.drafts || row < 0 || row >= pp.total_q) return;
-  const int kv = pp.group.of(head);
-  const int col = i * pp.group.d + head - kv * pp.group.d;
-  const int tile = col / kCols;
+  const int cols = s.drafts * pp.group.d;
+  if (t16 * kJoinCols >= cols) return;
+  const int tile = t16 * kJoinCols / kCols;
   const int64_t first = pp.before[b] + ((int64_t)tile * pp.hkv + kv) * s.blocks;
   const int64_t quota = pp.before[pp.num_seqs];
   const int64_t r0 = first / quota, r1 = (first + s.blocks - 1) / quota;
   if (r0 == r1) return;  // its workgroup has written it
-  // where a range begins with the item its partial output is the first of two
-  auto part_of = [&](int64_t r) {
-    return (2 * r + (r == r0 && first != r0 * quota ? 1 : 0)) * kCols + (col - tile * kCols);
-  };
-  OutT* const dst = out + (row * pp.hq + head) * kHeadDim + 2 * lane;
-  auto store = [&](float a, float b2) {
-    if constexpr (sizeof(OutT) == 4)
-      *reinterpret_cast<float2*>(dst) = make_float2(a, b2);
-    else
-      *reinterpret_cast<uint32_t*>(dst) = pack_bf16x2(a, b2);
-  };
-  if (pp.ml_ws[part_of(r1)].x == INFINITY) return store(0.f, 0.f);  // padding
-  float top = -INFINITY;
-  for (int64_t r = r0 + lane; r <= r1; r += 64) top = fmaxf(top, pp.ml_ws[part_of(r)].x);
+  const int row0 = pp.q_starts[b];
+  const int d = (threadIdx.x & 31) * 4;
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
-  float x = 0.f, y = 0.f, sum = 0.f;
-  for (int64_t base = r0; base <= r1; base += 64) {
-    const int64_t mine = base + lane;
-    const float2 ml = mine <= r1 ? pp.ml_ws[part_of(mine)] : make_float2(-INFINITY, 0.f);
-    const float weight = ml.x > -INFINITY ? fast_exp2(ml.x - top) : 0.f;
-    float l = ml.y * weight;
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off);
-    sum += l;
-    const int here = r1 - base < 63 ? (int)(r1 - base) + 1 : 64;
-    for (int j = 0; j < here; ++j) {
-      const float2 o = *reinterpret_cast<const float2*>(pp.o_ws + part_of(base + j) * kHeadDim + 2 * lane);
-      const float w = __shfl(weight, j);
-      x = w > 0.f ? fmaf(w, o.x, x) : x;
-      y = w > 0.f ? fmaf(w, o.y, y) : y;
+  for (int j = (int)threadIdx.x >> 5; j < kJoinCols; j += kJoinThreads / 32) {
+    const int col = t16 * kJoinCols + j;
+    if (col >= cols) continue;
+    const int qi = pp.group.of(col);
+    const int64_t row = (int64_t)row0 + qi;
+    if (row < 0 || row >= pp.total_q) continue;
+    OutT* const dst = out + (row * pp.hq + kv * pp.group.d + (col - qi * pp.group.d)) * kHeadDim + d;
+    // where a range begins with the item its partial output is the first of two
+    auto part_of = [&](int64_t r) {
+      return (2 * r + (r == r0 && first != r0 * quota ? 1 : 0)) * kCols + (col - tile * kCols);
+    };
+    float top = -INFINITY;
+    for (int64_t r = r0; r <= r1; ++r) top = fmaxf(top, pp.ml_ws[part_of(r)].x);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    if (top < INFINITY) {  // otherwise padding, which the last range has marked
+#pragma unroll 4
+      for (int64_t r = r0; r <= r1; ++r) {
+        const float2 ml = pp.ml_ws[part_of(r)];
+        const float w = ml.x > -INFINITY ? fast_exp2(ml.x - top) : 0.f;
+        const f32x4 x = *reinterpret_cast<const f32x4*>(pp.o_ws + part_of(r) * kHeadDim + d);
+        sum = fmaf(w, ml.y, sum);
+        if (w > 0.f) o += w * x;
+      }
     }
+    store4<OutT>(dst, o * (sum != 0.f ? 1.0f / sum : 0.f));
   }
-  const float inv = sum != 0.f ? 1.0f / sum : 0.f;
-  store(x * inv, y * inv);
 }
 
 // ------------------------------------------------------------ host
 
 // Waves and tiles of a workgroup, and the ranges of a call.
 struct Shape {
-  int waves, tiles;
+  int col_waves, tiles;
   int32_t ranges;
-  int cols() const { return waves * tiles * 16; }
+  int cols() const { return col_waves * tiles * 16; }
   int64_t parts() const { return 2 * (int64_t)ranges * cols(); }
   size_t o_bytes() const { return (size_t)parts() * kHeadDim * sizeof(float); }
   size_t ml_bytes() const { return (size_t)parts() * sizeof(float2); }
@@ -719,14 +763,13 @@ Shape shape_of(const ctx_decode_attn* h, int32_t num_seqs, int32_t max_q_len) {
   const ctx_decode_attn_desc& d = h->desc;
   const int64_t cols = (int64_t)max_q_len * (d.num_q_heads / d.num_kv_heads);
   Shape s;
-  s.waves = cols <= 64 ? 4 : 8;
-  s.tiles = cols <= 128 ? 1 : 2;
-  // no more ranges than the longest sequences have parts of kLeastBlocks blocks
-  const int64_t resident = (int64_t)h->num_cus * (s.waves == 4 ? 3 : s.tiles == 1 ? 2 : 1);
+  s.col_waves = cols <= 128 ? 4 : 8;
+  s.tiles = cols <= 64 ? 1 : 2;
+  // a workgroup per CU, but no more ranges than the longest sequences have parts of kLeastBlocks blocks
   const int64_t items = (int64_t)num_seqs * d.num_kv_heads * ((cols + s.cols() - 1) / s.cols());
   const int64_t blocks = ((int64_t)d.max_seq_len + kBlock - 1) / kBlock;
   const int64_t most = (items * blocks + kLeastBlocks - 1) / kLeastBlocks;
-  const int64_t ranges = most < resident ? most : resident;
+  const int64_t ranges = most < h->num_cus ? most : h->num_cus;
   s.ranges = ranges > 1 ? (int32_t)ranges : 1;
   return s;
 }
@@ -735,8 +778,8 @@ int check_drafts(const ctx_decode_attn* h, int32_t num_seqs, int32_t max_q_len) 
   if (h->desc.page_tokens <= 0) return fail(CTX_ERR_UNSUPPORTED, "the handle was created without page_tokens");
   if (max_q_len < 0) return fail(CTX_ERR_INVALID_ARG, "max_q_len %d < 0", max_q_len);
   if (max_q_len > kMostDrafts) return fail(CTX_ERR_UNSUPPORTED, "max_q_len %d > %d", max_q_len, kMostDrafts);
-  if ((int64_t)num_seqs * max_q_len * h->desc.num_q_heads > (int64_t)kMostTokens * kJoinWaves)
-    return fail(CTX_ERR_INVALID_ARG, "tree grid too large");
+  const int64_t tiles = ((int64_t)max_q_len * (h->desc.num_q_heads / h->desc.num_kv_heads) + kJoinCols - 1) / kJoinCols;
+  if (tiles * num_seqs * h->desc.num_kv_heads > kMostTokens) return fail(CTX_ERR_INVALID_ARG, "tree grid too large");
   return CTX_OK;
 }
 
@@ -747,22 +790,23 @@ struct TreeArgs {
   hipStream_t stream;
 };
 
-template <typename OutT, int kTerms, int kChange, int kWaves, int kTiles>
+template <typename OutT, int kTerms, int kChange, int kColWaves, int kTiles>
 void launch_shape(const TreeArgs& a) {
-  constexpr int kCols = kColsOf<kWaves, kTiles>;
-  hipLaunchKernelGGL((tree_attn_kernel<OutT, kTerms, kChange, kWaves, kTiles>), dim3((unsigned)a.plan.ranges),
+  constexpr int kCols = kColsOf<kColWaves, kTiles>;
+  hipLaunchKernelGGL((tree_attn_kernel<OutT, kTerms, kChange, kColWaves, kTiles>), dim3((unsigned)a.plan.ranges),
                      dim3(64 * kWaves), 0, a.stream, a.q, a.k, a.v, a.plan, static_cast<OutT*>(a.out));
-  const int64_t parts = (int64_t)a.plan.num_seqs * a.plan.max_q_len * a.plan.hq;
-  hipLaunchKernelGGL((tree_join_kernel<OutT, kCols>), dim3((unsigned)((parts + kJoinWaves - 1) / kJoinWaves)),
-                     dim3(64 * kJoinWaves), 0, a.stream, a.plan, static_cast<OutT*>(a.out));
+  const int tiles16 = (a.plan.max_q_len * a.plan.group.d + kJoinCols - 1) / kJoinCols;
+  const int64_t grid = (int64_t)tiles16 * a.plan.num_seqs * a.plan.hkv;
+  hipLaunchKernelGGL((tree_join_kernel<OutT, kCols>), dim3((unsigned)grid), dim3(kJoinThreads), 0, a.stream, a.plan,
+                     tiles16, static_cast<OutT*>(a.out));
 }
 
 template <typename OutT, int kTerms, int kChange>
 void launch_change(const TreeArgs& a, const Shape& s) {
-  if (s.waves == 4)
+  if (s.tiles == 1)
     launch_shape<OutT, kTerms, kChange, 4, 1>(a);
-  else if (s.tiles == 1)
-    launch_shape<OutT, kTerms, kChange, 8, 1>(a);
+  else if (s.col_waves == 4)
+    launch_shape<OutT, kTerms, kChange, 4, 2>(a);
   else
     launch_shape<OutT, kTerms, kChange, 8, 2>(a);
 }
