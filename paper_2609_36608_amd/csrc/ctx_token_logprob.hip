@@ -159,13 +159,24 @@ __device__ __forceinline__ uint64_t key_of(float z, int32_t column) {
   return (uint64_t)order_of(z) << 32 | (uint32_t)~column;
 }
 
-// how many of keys[0 .. n) are larger
-__device__ __forceinline__ int rank_of(uint64_t key, const uint64_t* keys, int n) {
-  int r = 0;
-#pragma unroll 4
-  for (int i = 0; i < n; ++i) r += keys[i] > key ? 1 : 0;
-  return r;
+// How many of keys[0 .. n) are larger than each of two; n a multiple of 8, keys 16-byte aligned,
+// zeros behind the last.
+__device__ __forceinline__ void ranks_of(uint64_t k0, uint64_t k1, const uint64_t* keys, int n, int& r0, int& r1) {
+  typedef unsigned long long u64x2 __attribute__((ext_vector_type(2)));
+  r0 = r1 = 0;
+  for (int i = 0; i < n; i += 8) {
+    u64x2 k[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const u64x2*>(keys + i + 2 * j);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      r0 += (k[j].x > k0 ? 1 : 0) + (k[j].y > k0 ? 1 : 0);
+      r1 += (k[j].x > k1 ? 1 : 0) + (k[j].y > k1 ? 1 : 0);
+    }
+  }
 }
+
+constexpr int round8(int n) { return (n + 7) & -8; }
 
 // A wave's alternatives: keys[0 .. count), of which any may be among the best `top`, and a
 // key that others must pass to be.  A wave goes through its columns in rising order from one
@@ -181,13 +192,11 @@ struct Best {
 __device__ __forceinline__ void cut(Best& b, int top, int lane) {
   wave_lds_fence();
   const uint64_t k0 = lane < b.count ? b.keys[lane] : 0, k1 = lane + 64 < b.count ? b.keys[lane + 64] : 0;
-  int r0 = 0, r1 = 0;
-#pragma unroll 4
-  for (int i = 0; i < b.count; ++i) {
-    const uint64_t k = b.keys[i];
-    r0 += k > k0 ? 1 : 0;
-    r1 += k > k1 ? 1 : 0;
-  }
+  const int n = (b.count + 7) & -8;
+  if (lane < n - b.count) b.keys[b.count + lane] = 0;
+  wave_lds_fence();
+  int r0, r1;
+  ranks_of(k0, k1, b.keys, n, r0, r1);
   wave_lds_fence();
   if (lane < b.count && r0 < top) b.keys[r0] = k0;
   if (lane + 64 < b.count && r1 < top) b.keys[r1] = k1;
@@ -214,7 +223,8 @@ __device__ __forceinline__ uint64_t first_key(float z, uint64_t* keys, int top, 
   const uint64_t key = key_of(z, lane);
   keys[lane] = key;
   wave_lds_fence();
-  const int r = rank_of(key, keys, 64);
+  int r, none;
+  ranks_of(key, ~0ull, keys, 64, r, none);
   wave_lds_fence();
   const unsigned long long who = __ballot(r == top - 1);
   const float at = __shfl(z, __builtin_ctzll(who));
@@ -269,28 +279,34 @@ __device__ __forceinline__ void write_row(const RowsArgs& a, int row, const Sums
   }
 }
 
-// The alternatives among keys[0 .. n) in LDS; 0 is none.
+// The alternatives among keys[0 .. n) in LDS, n a multiple of 8; 0 is none.  Places past the
+// last alternative have been filled by fill_top.
 __device__ __forceinline__ void write_top(const RowsArgs& a, int row, const Sums& sums, const uint64_t* keys, int n,
                                           int tid) {
-  const bool broken = is_broken(sums);
+  if (is_broken(sums)) return;
   const float log_s = __log2f(sums.s);
   const int64_t at = (int64_t)row * a.top;
-  int there = 0;
-  for (int i = 0; i < n; ++i) there += keys[i] != 0 ? 1 : 0;
+  for (int i = tid; i < n; i += 2 * kThreads) {
+    const uint64_t k0 = keys[i], k1 = i + kThreads < n ? keys[i + kThreads] : 0;
+    int r0, r1;
+    ranks_of(k0, k1, keys, n, r0, r1);
+    auto put = [&](uint64_t key, int r) {
+      if (key == 0 || r >= a.top) return;
+      a.top_tokens[at + r] = (int32_t) ~(uint32_t)key;
+      a.top_logp[at + r] = fmaf(value_of((uint32_t)(key >> 32)) - sums.m, a.scale, -log_s * kLn2);
+    };
+    put(k0, r0);
+    put(k1, r1);
+  }
+}
+
+// the places that `there` alternatives leave
+__device__ __forceinline__ void fill_top(const RowsArgs& a, int row, const Sums& sums, int there, int tid) {
+  const bool broken = is_broken(sums);
   if (broken) there = 0;
-  for (int i = tid; i < a.top; i += kThreads)
-    if (i >= there) {
-      a.top_tokens[at + i] = -1;
-      a.top_logp[at + i] = broken ? NAN : -INFINITY;
-    }
-  if (broken) return;
-  for (int i = tid; i < n; i += kThreads) {
-    const uint64_t key = keys[i];
-    if (key == 0) continue;
-    const int r = rank_of(key, keys, n);
-    if (r >= a.top) continue;
-    a.top_tokens[at + r] = (int32_t) ~(uint32_t)key;
-    a.top_logp[at + r] = fmaf(value_of((uint32_t)(key >> 32)) - sums.m, a.scale, -log_s * kLn2);
+  if (tid >= there && tid < a.top) {
+    a.top_tokens[(int64_t)row * a.top + tid] = -1;
+    a.top_logp[(int64_t)row * a.top + tid] = broken ? NAN : -INFINITY;
   }
 }
 
@@ -310,8 +326,9 @@ template <typename T, bool kTop, bool kEntropy>
 __global__ __launch_bounds__(kThreads) void logprob_kernel(RowsArgs a) {
   constexpr int kElems = kChunkOf<T>;
   __shared__ Sums lds_sums[kWaves];
-  __shared__ uint64_t lds_keys[kTop ? kWaves * kHeldKeys : 1];
-  __shared__ uint64_t lds_best[kTop ? kWaves * kMostTop : 1];
+  __shared__ __attribute__((aligned(16))) uint64_t lds_keys[kTop ? kWaves * kHeldKeys : 1];
+  __shared__ __attribute__((aligned(16))) uint64_t lds_best[kTop ? kWaves * kMostTop : 1];
+  __shared__ int lds_there[kWaves];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int row = (int)blockIdx.x / a.splits;
@@ -402,7 +419,8 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(RowsArgs a) {
   if (lane == 0) lds_sums[wave] = sums;
   if constexpr (kTop) {
     cut(best, a.top, lane);
-    if (lane < a.top) lds_best[wave * a.top + lane] = lane < best.count ? best.keys[lane] : 0;
+    if (lane < round8(a.top)) lds_best[wave * round8(a.top) + lane] = lane < best.count ? best.keys[lane] : 0;
+    if (lane == 0) lds_there[wave] = best.count;
   }
   __syncthreads();
   float m = lds_sums[0].m;
@@ -418,7 +436,13 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(RowsArgs a) {
   }
   if (a.splits == 1) {
     write_row<T>(a, row, all, tid);
-    if constexpr (kTop) write_top(a, row, all, lds_best, kWaves * a.top, tid);
+    if constexpr (kTop) {
+      int there = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) there += lds_there[w];
+      fill_top(a, row, all, there, tid);
+      write_top(a, row, all, lds_best, kWaves * round8(a.top), tid);
+    }
     return;
   }
   if (tid == 0) a.part[(int64_t)row * a.splits + split] = make_float4(all.m, all.s, all.t, 0.f);
@@ -426,38 +450,64 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(RowsArgs a) {
     // the share's best, in order
     uint64_t* const out = a.keys + ((int64_t)row * a.splits + split) * a.top;
     int there = 0;
-    for (int i = 0; i < kWaves * a.top; ++i) there += lds_best[i] != 0 ? 1 : 0;
-    for (int i = tid; i < kWaves * a.top; i += kThreads) {
-      const uint64_t key = lds_best[i];
-      if (key == 0) continue;
-      const int r = rank_of(key, lds_best, kWaves * a.top);
-      if (r < a.top) out[r] = key;
-    }
-    for (int i = tid; i < a.top; i += kThreads)
-      if (i >= there) out[i] = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) there += lds_there[w];
+    if (tid >= there && tid < a.top) out[tid] = 0;
+    const int n = kWaves * round8(a.top);  // up to a key per thread
+    const uint64_t key = tid < n ? lds_best[tid] : 0;
+    int r, none;
+    ranks_of(key, ~0ull, lds_best, n, r, none);
+    if (key != 0 && r < a.top) out[r] = key;
   }
 }
 
-// Joins a row's shares: one workgroup per row, a share per lane.
+// Joins a row's shares: one workgroup per row, a share per lane.  Of the shares' alternatives, each
+// share's in order, only those are compared with each other that reach a key which `top` of
+// them reach: with p = ceil(top / shares), the least of the shares' p-th ones, or the largest of
+// their last.
 template <typename T, bool kTop>
 __global__ __launch_bounds__(kThreads) void logprob_merge_kernel(RowsArgs a) {
-  __shared__ uint64_t lds_best[kTop ? kMostSplits * kMostTop : 1];
+  __shared__ __attribute__((aligned(16))) uint64_t lds_best[kTop ? kMostSplits * kMostTop + 8 : 1];
+  __shared__ int lds_count;
   const int tid = threadIdx.x, lane = tid & 63;
   const int row = blockIdx.x;
   if (a.mask != nullptr && a.mask[row] == 0) return write_masked(a, row, tid);
   const int64_t at = (int64_t)row * a.splits;
   Sums sums{kFloor, 0.f, 0.f};
+  uint64_t enough = 0, last = 0;
   if (lane < a.splits) {
     const float4 p = a.part[at + lane];
     sums = Sums{p.x, p.y, p.z};
+    if constexpr (kTop) {
+      const uint64_t* const keys = a.keys + (at + lane) * a.top;
+      enough = keys[(a.top + a.splits - 1) / a.splits - 1];
+      last = keys[a.top - 1];
+    }
   }
   sums = wave_join(sums, a.factor);
   write_row<T>(a, row, sums, tid);
   if constexpr (kTop) {
-    const int n = a.splits * a.top;
-    for (int i = tid; i < n; i += kThreads) lds_best[i] = a.keys[at * a.top + i];
+    if (lane >= a.splits) enough = ~0ull;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) {
+      const uint64_t e = __shfl_xor(enough, off), l = __shfl_xor(last, off);
+      enough = e < enough ? e : enough;
+      last = l > last ? l : last;
+    }
+    const uint64_t least = enough > last ? enough : last;
+    if (tid == 0) lds_count = 0;
     __syncthreads();
-    write_top(a, row, sums, lds_best, n, tid);
+    const int n = a.splits * a.top;
+    for (int base = 0; base < n; base += kThreads) {
+      const uint64_t key = base + tid < n ? a.keys[at * a.top + base + tid] : 0;
+      if (key != 0 && key >= least) lds_best[atomicAdd(&lds_count, 1)] = key;  // in any order
+    }
+    __syncthreads();
+    const int there = lds_count;
+    if (tid < 8) lds_best[there + tid] = 0;
+    __syncthreads();
+    fill_top(a, row, sums, there, tid);
+    write_top(a, row, sums, lds_best, (there + 7) & -8, tid);
   }
 }
 
