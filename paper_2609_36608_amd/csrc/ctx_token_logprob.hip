@@ -27,6 +27,7 @@
 #include <cstdarg>
 #include <cstdint>
 #include <cstdio>
+#include <type_traits>
 
 #include "ctx_token_logprob.h"
 
@@ -237,8 +238,21 @@ struct Sums {
   float m, s, t;
 };
 
+// What a difference to m is taken from: m's product with the factor, rounded, so that d is one FMA of
+// the logit.  What the rounding adds to every d of m alike cancels, since raise() takes differences of the
+// same rounded products; from 2^30 on it may be more than 2^d holds, and d is (z - m) factor
+// instead.
+constexpr float kLargeProduct = 1073741824.f;
+
+__device__ __forceinline__ bool is_large(float m, float factor) { return !(fabsf(m * factor) < kLargeProduct); }
+
+__device__ __forceinline__ float difference(float z, float m, float factor) {
+  return is_large(m, factor) ? (z - m) * factor : fmaf(z, factor, -(m * factor));
+}
+
 __device__ __forceinline__ void raise(Sums& a, float m, float factor) {
-  const float d = fminf((m - a.m) * factor, -kLeast);
+  const float by = is_large(m, factor) ? (m - a.m) * factor : m * factor - a.m * factor;
+  const float d = fminf(by, -kLeast);
   const float c = exp2_of(-d);
   a.t = c * fmaf(-d, a.s, a.t);
   a.s *= c;
@@ -256,6 +270,12 @@ __device__ __forceinline__ Sums wave_join(Sums a, float factor) {
 __device__ __forceinline__ bool is_broken(const Sums& a) { return !(a.m < INFINITY); }
 __device__ __forceinline__ bool is_empty(const Sums& a) { return a.m <= kFloor; }
 
+__device__ __forceinline__ float log_prob(const RowsArgs& a, float z, const Sums& sums, float log_s) {
+  const float d = difference(z, sums.m, a.factor);
+  // differences past fp32's range in log2 units alone
+  return d > -1e37f ? (d - log_s) * kLn2 : (z - sums.m) * a.scale;
+}
+
 // The row's outputs but for the alternatives; every thread has the sums.
 template <typename T>
 __device__ __forceinline__ void write_row(const RowsArgs& a, int row, const Sums& sums, int tid) {
@@ -268,7 +288,7 @@ __device__ __forceinline__ void write_row(const RowsArgs& a, int row, const Sums
       lp = NAN;
     } else if (tok >= 0) {
       const float z = value<T>(reinterpret_cast<const T*>(a.logits) + (int64_t)row * a.stride, tok);
-      lp = broken ? NAN : empty || z <= kFloor ? -INFINITY : fmaf(z - sums.m, a.scale, -log_s * kLn2);
+      lp = broken ? NAN : empty || z <= kFloor ? -INFINITY : log_prob(a, z, sums, log_s);
     }
     a.token_logp[(int64_t)row * a.num_tokens + tid] = lp;
   }
@@ -293,7 +313,7 @@ __device__ __forceinline__ void write_top(const RowsArgs& a, int row, const Sums
     auto put = [&](uint64_t key, int r) {
       if (key == 0 || r >= a.top) return;
       a.top_tokens[at + r] = (int32_t) ~(uint32_t)key;
-      a.top_logp[at + r] = fmaf(value_of((uint32_t)(key >> 32)) - sums.m, a.scale, -log_s * kLn2);
+      a.top_logp[at + r] = log_prob(a, value_of((uint32_t)(key >> 32)), sums, log_s);
     };
     put(k0, r0);
     put(k1, r1);
@@ -390,9 +410,10 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(RowsArgs a) {
     if constexpr (kTop) {
       if (fresh) best.key = first_key(top, best.keys, a.top, lane);
       fresh = false;
+      const bool some = __any(top > best.least());
 #pragma unroll
       for (int r = 0; r < kTileLoads; ++r) {
-        if (!__any(most[r] > best.least())) continue;
+        if (!some || !__any(most[r] > best.least())) continue;
         float z[kElems];
         unpack<T>(x[r], z);
         const int c = first + (r * 64 + lane) * kElems;
@@ -400,19 +421,38 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(RowsArgs a) {
         for (int e = 0; e < kElems; ++e) offer(best, z[e], c + e, a.top, lane);
       }
     }
+    // The sums of a tile.  A masked logit's d of -inf would make t NaN, which the lanes of such
+    // tiles have and take the sums again with d bounded; the others save a bound per logit.
+    auto add = [&](auto large, auto bounded, float& s, float& t) __attribute__((always_inline)) {
+      const float product = sums.m * factor;
 #pragma unroll
-    for (int r = 0; r < kTileLoads; ++r) {
-      float z[kElems];
-      unpack<T>(x[r], z);
+      for (int r = 0; r < kTileLoads; ++r) {
+        float z[kElems];
+        unpack<T>(x[r], z);
 #pragma unroll
-      for (int e = 0; e < kElems; ++e) {
-        float d = (z[e] - sums.m) * factor;
-        if (kEntropy) d = fmaxf(d, kLeast);
-        const float w = exp2_of(d);
-        sums.s += w;
-        if (kEntropy) sums.t = fmaf(w, d, sums.t);
+        for (int e = 0; e < kElems; ++e) {
+          float d = large ? (z[e] - sums.m) * factor : fmaf(z[e], factor, -product);
+          if (bounded) d = fmaxf(d, kLeast);
+          const float w = exp2_of(d);
+          s += w;
+          if (kEntropy) t = fmaf(w, d, t);
+        }
       }
+    };
+    float s = 0.f, t = 0.f;
+    const std::true_type yes;
+    const std::false_type no;
+    if (!__any(is_large(sums.m, factor))) {
+      add(no, no, s, t);
+      if (kEntropy && __any(t != t)) {
+        s = t = 0.f;
+        add(no, yes, s, t);
+      }
+    } else {
+      add(yes, yes, s, t);
     }
+    sums.s += s;
+    sums.t += t;
   }
 
   sums = wave_join(sums, factor);
@@ -567,7 +607,12 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(GradArgs a) {
   const float h = kEntropy && live ? a.entropy[row] : 0.f;
   const float c0 = st.x == st.x ? -a.scale * (kEntropy ? fmaf(by_h, h, by) : by) : NAN;
   const float c1 = kEntropy ? -a.scale * by_h * kLn2 : 0.f;
-  auto log2_p = [&](float z) __attribute__((always_inline)) { return fmaxf(fmaf(z - st.x, a.factor, -log_s), kLeast); };
+  const float product = st.x * a.factor;
+  const bool large = is_large(st.x, a.factor);
+  // log2 of a probability
+  auto log2_p = [&](float z) __attribute__((always_inline)) {
+    return fmaxf((large ? (z - st.x) * a.factor : fmaf(z, a.factor, -product)) - log_s, kLeast);
+  };
   auto weight = [&](float z) __attribute__((always_inline)) {
     const float d = log2_p(z);
     return exp2_of(d) * (kEntropy ? fmaf(c1, d, c0) : c0);
@@ -683,10 +728,12 @@ int query_cus(int* cus) {
   return CTX_OK;
 }
 
-// Workgroups that share a row: with few rows enough to fill the chip, a tile per wave at least.
+// Workgroups that share a row: kPerCu of them per CU in all, a tile per wave at least.
+constexpr int kPerCu = 8;
+
 int32_t splits_of(ctx_dtype dtype, int32_t vocab, int32_t rows, int cus) {
   const int64_t tiles = ((int64_t)vocab + chunk_of(dtype) * kTileChunks - 1) / (chunk_of(dtype) * kTileChunks);
-  const int64_t want = (4 * (int64_t)cus + rows - 1) / rows;
+  const int64_t want = (kPerCu * (int64_t)cus + rows - 1) / rows;
   int64_t s = tiles / kWaves;
   s = s < want ? s : want;
   s = s < kMostSplits ? s : kMostSplits;
@@ -799,8 +846,6 @@ extern "C" int ctx_token_logprob_grad_run(const void* logits, ctx_dtype dtype, i
     return fail(CTX_ERR_INVALID_ARG, "entropy and grad_entropy must both be given or both be NULL");
   if (!aligned16(logits) || !aligned16(grad_logits))
     return fail(CTX_ERR_ALIGNMENT, "logits and grad_logits must be 16-byte aligned");
-  int cus = 0;
-  if ((rc = query_cus(&cus)) != CTX_OK) return rc;
   GradArgs a{};
   a.logits = logits;
   a.grad = grad_logits;
@@ -816,7 +861,13 @@ extern "C" int ctx_token_logprob_grad_run(const void* logits, ctx_dtype dtype, i
   a.entropy = entropy;
   a.grad_logp = grad_logp;
   a.grad_entropy = grad_entropy;
-  a.splits = splits_of(dtype, vocab, num_rows, cus);
+  // A workgroup per tile of a row: all of them at work at once read and write near each other, as
+  // a copy does (2,057 rows of 151,936 bf16 logits 195 us, with 4 workgroups per row 250; smaller
+  // tiles gain nothing: half 203).
+  const int64_t chunks = (vocab + chunk_of(dtype) - 1) / chunk_of(dtype);
+  const int64_t tiles = (chunks + kTileLoads * kThreads - 1) / (kTileLoads * kThreads);
+  const int64_t most = ((int64_t)1 << 30) / num_rows;
+  a.splits = (int32_t)(tiles < most ? tiles : most);
   const dim3 grid((unsigned)num_rows * (unsigned)a.splits), block(kThreads);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (dtype == CTX_DTYPE_BF16) {
