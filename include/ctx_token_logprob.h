@@ -28,7 +28,7 @@
  *
  * Arithmetic: fp32 (differences to the largest logit in one FMA each, sums over lanes and
  * then in a fixed order); gradients are rounded to the logits' type once, nearest even.
- * Deterministic, no atomics.
+ * Deterministic.
  *
  * Conventions as in ctx_decode_attn.h: device pointers unless stated, owned by the
  * caller until the work queued on `stream` completes; asynchronous, no allocation,
@@ -91,7 +91,7 @@ int ctx_token_logprob_run(const void* logits, ctx_dtype dtype, int64_t row_strid
  *   grad_logp     float [num_rows, num_tokens]: a (NULL with num_tokens = 0)
  *   entropy, grad_entropy  float [num_rows]: that call's, and b; both NULL: b = 0
  *   grad_logits   `dtype` [num_rows, grad_row_stride] out; columns >= vocab are not
- *                 written.  It may not overlap the logits
+ *                 written.  It may not overlap the logits (INVALID_ARG)
  * A row whose sum of a and whose b are 0, and whose tokens' gradients all are, gets zeros
  * without being read.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT (16 bytes: logits,
  * grad_logits), HIP.

@@ -901,7 +901,7 @@ def token_logprobs(logits, tokens=None, mask=None, temperature: float = 1.0, top
 
     logits bf16 or float32 [N, V] (rows may be views of wider ones, a multiple of 16 bytes apart),
     tokens int32 [N] or [N, M] (M up to 64; below 0: none), mask uint8 [N] (0: the row is not read).
-    Returns a dict of device tensors: token_logp float32 like tokens, entropy [N] (with entropy=True),
+    Returns a dict of device tensors: token_logp float32 like tokens (if M > 0), entropy [N] (with entropy=True),
     top_tokens int32 and top_logp [N, top] (the lowest column first among equal logits, -1 where there
     is none) and stats [N, 2], which token_logprobs_grad takes.  Tensors given in `out` under those
     names are written in place; the others, and the workspace of a call on few rows (uint8), are

@@ -715,6 +715,16 @@ int check_tokens(const int32_t* tokens, int32_t num_tokens) {
   return CTX_OK;
 }
 
+// Whether two arrays of rows of `width` bytes share any: rows of equal strides may lie between each
+// other's.
+bool rows_overlap(const void* p, int64_t p_stride, const void* q, int64_t q_stride, int64_t width, int64_t rows) {
+  const int64_t a = (int64_t)reinterpret_cast<uintptr_t>(p), b = (int64_t)reinterpret_cast<uintptr_t>(q);
+  if (a + (rows - 1) * p_stride + width <= b || b + (rows - 1) * q_stride + width <= a) return false;
+  if (p_stride != q_stride || rows == 1) return true;
+  const int64_t off = ((b - a) % p_stride + p_stride) % p_stride;
+  return off < width || off + width > p_stride;
+}
+
 int check_scale(float scale) {
   if (!(scale >= 1e-30f && scale <= 1e30f)) return fail(CTX_ERR_INVALID_ARG, "scale must be in [1e-30, 1e30]");
   return CTX_OK;
@@ -846,6 +856,9 @@ extern "C" int ctx_token_logprob_grad_run(const void* logits, ctx_dtype dtype, i
     return fail(CTX_ERR_INVALID_ARG, "entropy and grad_entropy must both be given or both be NULL");
   if (!aligned16(logits) || !aligned16(grad_logits))
     return fail(CTX_ERR_ALIGNMENT, "logits and grad_logits must be 16-byte aligned");
+  const int64_t size = 16 / chunk_of(dtype);
+  if (rows_overlap(logits, row_stride * size, grad_logits, grad_row_stride * size, vocab * size, num_rows))
+    return fail(CTX_ERR_INVALID_ARG, "grad_logits overlaps the logits");
   GradArgs a{};
   a.logits = logits;
   a.grad = grad_logits;

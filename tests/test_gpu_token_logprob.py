@@ -332,6 +332,23 @@ def test_outputs_and_what_lies_behind_them():
         assert torch.allclose(one[k].float(), want[k][3:4].float(), rtol=1e-5, atol=1e-5), k
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_gradients_between_the_logits(dtype):
+    """Logits and gradients are column slices of the same rows."""
+    rows, vocab = 5, 1003
+    z = logits_of(14, rows, vocab, dtype, wide=2048)
+    tokens = torch.arange(rows, dtype=torch.int32).cuda()
+    result, by = token_logprobs(z, tokens), torch.ones(rows).cuda()
+    want = token_logprobs_grad(z, tokens, result, by)
+    both = torch.full((rows, 2048), 5.0, dtype=dtype, device="cuda")
+    both[:, :vocab] = z
+    token_logprobs_grad(both[:, :vocab], tokens, result, by, out=both[:, 1008:1008 + vocab])
+    assert torch.equal(both[:, 1008:1008 + vocab], want) and torch.equal(both[:, :vocab], z)
+    assert (both[:, vocab:1008] == 5.0).all() and (both[:, 1008 + vocab:] == 5.0).all()
+    with pytest.raises(bd.CtxError, match="overlaps"):
+        token_logprobs_grad(both[:, :vocab], tokens, result, by, out=both[:, 1000:1000 + vocab])
+
+
 def test_refusals():
     z = logits_of(1, 4, 96, torch.bfloat16)
     t = torch.zeros(4, dtype=torch.int32).cuda()

@@ -84,6 +84,20 @@ def test_grad_refuses(lib, kw, status):
     assert lib.ctx_decode_attn_last_error().decode()
 
 
+@pytest.mark.parametrize("kw", [
+    dict(grad_logits=4096),  # the logits themselves
+    dict(grad_logits=4096 + 192),  # the last 4 columns of a row
+    dict(grad_logits=4096 + 2 * 208 + 192, grad_row_stride=512),  # of the last one
+    dict(grad_logits=4096 - 400),
+    dict(row_stride=208, grad_row_stride=208, grad_logits=4096 + 416 + 192),  # between rows, not far enough
+    dict(num_rows=1, row_stride=2**20, grad_row_stride=2**20, grad_logits=4096 + 96),
+    dict(dtype=F32, grad_logits=4096 + 384),
+])
+def test_grad_refuses_to_overwrite_the_logits(lib, kw):
+    assert lib.ctx_token_logprob_grad_run(*grad_args(logits=4096, **kw).values()) == bd.CTX_ERR_INVALID_ARG
+    assert "overlaps" in lib.ctx_decode_attn_last_error().decode()
+
+
 def test_no_rows(lib):
     assert lib.ctx_token_logprob_run(*run_args(num_rows=0, logits=None, tokens=None, top_tokens=None).values()) == bd.CTX_OK
     assert lib.ctx_token_logprob_grad_run(*grad_args(num_rows=0, logits=None, stats=None).values()) == bd.CTX_OK
