@@ -252,9 +252,10 @@ __global__ __launch_bounds__(kPlanThreads) void resize_kernel(Resize a) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   for (int b = wave; b < a.rows.num_seqs; b += kPlanWaves) give_back(a, b, lane, 64);
-  // The counts change in L2, past this CU's cache, which holds none of them yet: what is read of
-  // them from here on is what the atomics, once they are done, have left.
+  // The counts change in L2, past this CU's cache, which may hold lines with some of them, read for
+  // lengths or tables beside them: once a wave's atomics are done it drops these lines.
   __builtin_amdgcn_s_waitcnt(0);
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   __syncthreads();
   plan(a, lds_scan);
   __builtin_amdgcn_s_waitcnt(0);

@@ -136,6 +136,34 @@ def test_pool_runs_out():
     assert pool.refs == [0] * 10
 
 
+@pytest.mark.parametrize("seqs,pages", [(6, 24), (20, 100), (64, 300)])
+def test_state_in_one_buffer(seqs, pages):
+    """Lengths, tables, counts and outputs right behind each other: what is counted shares cache lines
+    with what is read before, in either order."""
+    rng = np.random.default_rng(seqs)
+    width, page = 4, 16
+    for order in (["lens", "new", "refs", "table"], ["table", "refs", "new", "lens"], ["refs", "lens", "table", "new"]):
+        pool = Pool(seqs, width, page, pages)
+        sizes = dict(lens=seqs, new=seqs, refs=pages, table=seqs * width)
+        ws = (2 * seqs + pages + 3) // 4 * 4
+        state = torch.zeros(ws + sum(sizes.values()), dtype=torch.int32, device="cuda")
+        part, at = {}, ws
+        for name in order:
+            part[name] = state[at:at + sizes[name]]
+            at += sizes[name]
+        table = part["table"].view(seqs, width)
+        table.fill_(-1)
+        with DecodeAttention(2, 2, seqs, width * page, page_tokens=page) as attn:
+            for step in range(12):
+                new = rng.integers(0, width * page + 1, seqs).tolist()
+                part["new"].copy_(i32(new))
+                granted, copies = attn.resize_pages(table, part["lens"], part["new"], part["refs"], granted=part["lens"],
+                                                    workspace=state[:ws].view(torch.uint8))
+                want = pool.resize(new)
+                assert granted.tolist() == pool.lens and copies.tolist() == want, (order, step)
+                assert table.tolist() == pool.table and part["refs"].tolist() == pool.refs, (order, step)
+
+
 def test_no_pages_and_broken_tables():
     pool = Pool(3, 2, 16, 0)
     dev = OnDevice(pool)
