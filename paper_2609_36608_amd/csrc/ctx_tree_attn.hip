@@ -30,6 +30,7 @@
 #include <climits>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "ctx_attn_common.h"
 #include "ctx_paged_common.h"
@@ -112,6 +113,9 @@ __device__ __forceinline__ int64_t quota_of(int64_t total, int ranges) {
   const int64_t even = (total + ranges - 1) / ranges;
   return even > kLeastBlocks ? even : kLeastBlocks;
 }
+
+// A barrier after which the waves see each other's LDS writes.  Loads into LDS stay in flight.
+__device__ __forceinline__ void lds_sync() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 constexpr int kWaves = 8;
 constexpr int kStages = 4;  // of a step's blocks in LDS
@@ -240,58 +244,13 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kernel(const uint16_t* 
       // the tree, for blocks with drafts and where positions are asked for; the item's last
       // workgroup has it in any case, to know the padding
       const bool has_drafts = last_block == s.blocks || last_block * kBlock + s.skip > s.hist;
-      if (tree_of != b && (has_drafts || pp.window > 0 || kHasBias)) {
-        tree_of = b;
-        int up = -2;  // the ancestor 2^k above; -1: none, -2: padding
-        uint32_t mask[kWords];
-#pragma unroll
-        for (int w = 0; w < kWords; ++w) mask[w] = 0;
-        if (tid < s.drafts) {
-          const int64_t row = (int64_t)row0 + tid;
-          const int parent = row >= 0 && row < pp.total_q ? pp.parents[row] : -2;
-          up = parent >= -1 && parent < tid ? parent : -2;
-#pragma unroll
-          for (int w = 0; w < kWords; ++w) mask[w] = tid >> 5 == w ? 1u << (tid & 31) : 0u;
-        }
-        bool more = true;
-        while (more) {
-          __syncthreads();
-          if (tid < kNodes) {
-            lds_up[tid] = (int16_t)up;
-#pragma unroll
-            for (int w = 0; w < kWords; ++w) lds_mask[tid][w] = mask[w];
-          }
-          __syncthreads();
-          if (up >= 0) {
-#pragma unroll
-            for (int w = 0; w < kWords; ++w) mask[w] |= lds_mask[up][w];
-            up = lds_up[up];
-          }
-          more = __syncthreads_or(up >= 0) != 0;
-        }
-        int depth = -1;
-#pragma unroll
-        for (int w = 0; w < kWords; ++w) {
-          if (up == -2) mask[w] = 0;
-          depth += __builtin_popcount(mask[w]);
-        }
-        if (tid < kNodes) lds_depth[tid] = (int16_t)depth;
-        __syncthreads();
-        if (pp.window > 0 && depth >= pp.window) {  // ancestors past the window
-#pragma unroll
-          for (int w = 0; w < kWords; ++w)
-            for (uint32_t left = mask[w]; left != 0; left &= left - 1) {
-              const int a = w * 32 + __builtin_ctz(left);
-              if (depth - lds_depth[a] >= pp.window) mask[w] &= ~(left & -left);
-            }
-        }
-        if (tid < kNodes) {
-#pragma unroll
-          for (int w = 0; w < kWords; ++w) lds_mask[tid][w] = mask[w];
-        }
-        __syncthreads();
+      const bool need_tree = tree_of != b && (has_drafts || pp.window > 0 || kHasBias);
+      int up = -2;  // the ancestor 2^k above; -1: none, -2: padding
+      if (need_tree && tid < s.drafts) {
+        const int64_t row = (int64_t)row0 + tid;
+        const int parent = row >= 0 && row < pp.total_q ? pp.parents[row] : -2;
+        up = parent >= -1 && parent < tid ? parent : -2;
       }
-
       // this lane's columns
       auto row_at = [&](int ct) -> int64_t {  // first element of its query (and output) row, -1 without one
         const int col = tile * kCols + (ct * kColWaves + col_wave) * 16 + n;
@@ -299,48 +258,24 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kernel(const uint16_t* 
         const int64_t row = (int64_t)row0 + qi;
         return qi < s.drafts && row >= 0 && row < pp.total_q ? (row * pp.hq + kv * g + (col - qi * g)) * kHeadDim : -1;
       };
-      int draft[kTiles];  // -1 without one
-      int low[kTiles], pos[kTiles];
-      float slope[kTiles];
+      auto head_at = [&](int ct) {
+        const int col = tile * kCols + (ct * kColWaves + col_wave) * 16 + n;
+        return kv * g + (col - pp.group.of(col) * g);
+      };
       bf16x8 qb[kTiles][4];
-      bool padding[kTiles];
-      int all_low = 0;  // what every column of the wave sees past the prefix
+      float slope[kTiles];
 #pragma unroll
       for (int ct = 0; ct < kTiles; ++ct) {
-        const int col = tile * kCols + (ct * kColWaves + col_wave) * 16 + n;
-        const int qi = pp.group.of(col);
         const int64_t row = row_at(ct);
-        draft[ct] = -1;
-        low[ct] = 0;
-        pos[ct] = s.hist;
-        slope[ct] = 0.f;
-        padding[ct] = false;
-        if (row >= 0) {
-          draft[ct] = qi;
-          if (pp.window > 0 || kHasBias) {
-            const int depth = lds_depth[qi];
-            padding[ct] = depth < 0;
-            pos[ct] = s.hist + (depth < 0 ? 0 : depth);
-            if (pp.window > 0 && pos[ct] >= pp.window) low[ct] = pos[ct] - pp.window + 1;
-            if (kHasBias) slope[ct] = pp.slopes[kv * g + (col - qi * g)] * 1.4426950408889634f;
-          } else if (has_drafts) {
-            padding[ct] = lds_depth[qi] < 0;
-          }
-          all_low = low[ct] > all_low ? low[ct] : all_low;
-          const uint16_t* qrow = q + row + 8 * c;
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk) qb[ct][kk] = as_bf16x8(load16(qrow + 32 * kk));
-        } else {
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk) qb[ct][kk] = as_bf16x8(u32x4{0u, 0u, 0u, 0u});
-        }
+        for (int kk = 0; kk < 4; ++kk)
+          qb[ct][kk] = as_bf16x8(row >= 0 ? load16(q + row + 8 * c + 32 * kk) : u32x4{0u, 0u, 0u, 0u});
+        slope[ct] = kHasBias && row >= 0 ? pp.slopes[head_at(ct)] * 1.4426950408889634f : 0.f;
       }
-#pragma unroll
-      for (int off = 1; off < 16; off <<= 1) {
-        const int other = __shfl_xor(all_low, off);
-        all_low = other > all_low ? other : all_low;
-      }
-      all_low = __builtin_amdgcn_readfirstlane(all_low);
+      int draft[kTiles];  // -1 without one
+      int low[kTiles], pos[kTiles];
+      bool padding[kTiles];
+      int all_low = 0;  // what every column of the wave sees past the prefix
       const bool busy = pp.group.of(tile * kCols + col_wave * 16) < s.drafts;  // wave-uniform
 
       Softmax st[kTiles];
@@ -349,7 +284,6 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kernel(const uint16_t* 
 #pragma unroll
       for (int ct = 0; ct < kTiles; ++ct) {
         st[ct] = Softmax{0.f, 0.f};
-        if (kHasBias && slope[ct] < 0.f) st[ct].m = -slope[ct] * (float)pos[ct];  // near the largest bias
 #pragma unroll
         for (int nb = 0; nb < 8; ++nb) o[ct][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
@@ -616,9 +550,82 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kernel(const uint16_t* 
           values(vt + part_wave * kBlockElems, pt);
         }
       };
-      issue(first_block, lds_k0, lds_v0, 0);
-      issue(first_block + kStep, lds_k1, lds_v1, 1);
-      issue(first_block + 2 * kStep, lds_k2, lds_v2, 2);
+      auto start = [&]() __attribute__((always_inline)) {
+        issue(first_block, lds_k0, lds_v0, 0);
+        issue(first_block + kStep, lds_k1, lds_v1, 1);
+        issue(first_block + 2 * kStep, lds_k2, lds_v2, 2);
+      };
+      // blocks without drafts need no tree, and are on their way while it is built
+      const bool early = (int64_t)(first_block + 3 * kStep) * kBlock + s.skip <= s.hist;
+      if (early) start();
+      if (need_tree) {
+        tree_of = b;
+        uint32_t mask[kWords];
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) mask[w] = tid < s.drafts && tid >> 5 == w ? 1u << (tid & 31) : 0u;
+        for (int above = 1; above < s.drafts; above *= 2) {
+          if (tid < kNodes) {
+            lds_up[tid] = (int16_t)up;
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) lds_mask[tid][w] = mask[w];
+          }
+          lds_sync();
+          if (up >= 0) {
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) mask[w] |= lds_mask[up][w];
+            up = lds_up[up];
+          }
+          lds_sync();
+        }
+        int depth = -1;
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) {
+          if (up == -2) mask[w] = 0;
+          depth += __builtin_popcount(mask[w]);
+        }
+        if (tid < kNodes) lds_depth[tid] = (int16_t)depth;
+        lds_sync();
+        if (pp.window > 0 && depth >= pp.window) {  // ancestors past the window
+#pragma unroll
+          for (int w = 0; w < kWords; ++w)
+            for (uint32_t left = mask[w]; left != 0; left &= left - 1) {
+              const int a = w * 32 + __builtin_ctz(left);
+              if (depth - lds_depth[a] >= pp.window) mask[w] &= ~(left & -left);
+            }
+        }
+        if (tid < kNodes) {
+#pragma unroll
+          for (int w = 0; w < kWords; ++w) lds_mask[tid][w] = mask[w];
+        }
+        lds_sync();
+      }
+      if (!early) start();
+#pragma unroll
+      for (int ct = 0; ct < kTiles; ++ct) {
+        const int qi = pp.group.of(tile * kCols + (ct * kColWaves + col_wave) * 16 + n);
+        draft[ct] = row_at(ct) >= 0 ? qi : -1;
+        low[ct] = 0;
+        pos[ct] = s.hist;
+        padding[ct] = false;
+        if (draft[ct] >= 0) {
+          if (pp.window > 0 || kHasBias) {
+            const int depth = lds_depth[qi];
+            padding[ct] = depth < 0;
+            pos[ct] = s.hist + (depth < 0 ? 0 : depth);
+            if (pp.window > 0 && pos[ct] >= pp.window) low[ct] = pos[ct] - pp.window + 1;
+          } else if (has_drafts) {
+            padding[ct] = lds_depth[qi] < 0;
+          }
+          all_low = low[ct] > all_low ? low[ct] : all_low;
+        }
+        if (kHasBias && slope[ct] < 0.f) st[ct].m = -slope[ct] * (float)pos[ct];  // near the largest bias
+      }
+#pragma unroll
+      for (int off = 1; off < 16; off <<= 1) {
+        const int other = __shfl_xor(all_low, off);
+        all_low = other > all_low ? other : all_low;
+      }
+      all_low = __builtin_amdgcn_readfirstlane(all_low);
       // whole rounds of four steps; the last of them may be on empty blocks
       for (int u = first_block; u < last_block; u += kStages * kStep) {
         step(u, lds_k0, lds_v0, lds_k3, lds_v3);
@@ -696,54 +703,83 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kernel(const uint16_t* 
   }
 }
 
-// Joins the partial outputs of the items: a workgroup per 16-column tile of an item, 32 lanes of
-// 4 dimensions per column, in the order of ranges.
-constexpr int kJoinThreads = 256;
+// Joins the partial outputs of the items: a workgroup per 16 columns of an item, 16 lanes of twice
+// 4 dimensions per column.  Bound by the latency of its loads, so the lanes ask for the maxima
+// and sums of 16 ranges at once, and for several ranges' outputs.
 constexpr int kJoinCols = 16;
+constexpr int kJoinLanes = 16;
+constexpr int kJoinParts = kHeadDim / (4 * kJoinLanes);
+constexpr int kJoinThreads = kJoinCols * kJoinLanes;
 
 template <typename OutT, int kCols>
-__global__ __launch_bounds__(kJoinThreads) void tree_join_kernel(TreePlan pp, int tiles16, OutT* __restrict__ out) {
-  const int t16 = (int)blockIdx.x % tiles16;
-  const int unit = (int)blockIdx.x / tiles16;
+__global__ __launch_bounds__(kJoinThreads) void tree_join_kernel(TreePlan pp, int join_tiles, OutT* __restrict__ out) {
+  const int join_tile = (int)blockIdx.x % join_tiles;
+  const int unit = (int)blockIdx.x / join_tiles;
   const int b = unit / pp.hkv, kv = unit - b * pp.hkv;
   const Seen s = seen_of(pp, b);
-  const int cols = s.drafts * pp.group.d;
-  if (t16 * kJoinCols >= cols) return;
-  const int tile = t16 * kJoinCols / kCols;
-  const int64_t first = pp.before[b] + ((int64_t)tile * pp.hkv + kv) * s.blocks;
-  const int64_t quota = pp.before[pp.num_seqs];
-  const int64_t r0 = first / quota, r1 = (first + s.blocks - 1) / quota;
-  if (r0 == r1) return;  // its workgroup has written it
+  const int lane = threadIdx.x % kJoinLanes;
+  const int col = join_tile * kJoinCols + (int)threadIdx.x / kJoinLanes;
+  if (join_tile * kJoinCols >= s.drafts * pp.group.d) return;
   const int row0 = pp.q_starts[b];
-  const int d = (threadIdx.x & 31) * 4;
+  const int64_t quota = pp.before[pp.num_seqs];
+  const int tile = join_tile * kJoinCols / kCols;
+  const int64_t first = pp.before[b] + ((int64_t)tile * pp.hkv + kv) * s.blocks;
+  const int64_t r0 = first / quota;
+  const int ranges = (int)((first + s.blocks - 1) / quota - r0) + 1;
+  if (ranges == 1) return;  // its workgroup has written it
+  const int qi = pp.group.of(col);
+  const int64_t row = (int64_t)row0 + qi;
+  if (qi >= s.drafts || row < 0 || row >= pp.total_q) return;  // for all lanes of the column
+  // where a range begins with the item its partial output is the first of two
+  const int second = first != r0 * quota ? 1 : 0;
+  auto part_of = [&](int r) { return (2 * (r0 + r) + (r == 0 ? second : 0)) * kCols + (col - tile * kCols); };
+  const float2 none = make_float2(-INFINITY, 0.f);
+  float2 ml = lane < ranges ? pp.ml_ws[part_of(lane)] : none;  // of range base + lane
+  float top = ml.x;
+  for (int base = kJoinLanes; base < ranges; base += kJoinLanes)
+    top = fmaxf(top, base + lane < ranges ? pp.ml_ws[part_of(base + lane)].x : -INFINITY);
 #pragma unroll
-  for (int j = (int)threadIdx.x >> 5; j < kJoinCols; j += kJoinThreads / 32) {
-    const int col = t16 * kJoinCols + j;
-    if (col >= cols) continue;
-    const int qi = pp.group.of(col);
-    const int64_t row = (int64_t)row0 + qi;
-    if (row < 0 || row >= pp.total_q) continue;
-    OutT* const dst = out + (row * pp.hq + kv * pp.group.d + (col - qi * pp.group.d)) * kHeadDim + d;
-    // where a range begins with the item its partial output is the first of two
-    auto part_of = [&](int64_t r) {
-      return (2 * r + (r == r0 && first != r0 * quota ? 1 : 0)) * kCols + (col - tile * kCols);
-    };
-    float top = -INFINITY;
-    for (int64_t r = r0; r <= r1; ++r) top = fmaxf(top, pp.ml_ws[part_of(r)].x);
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
-    if (top < INFINITY) {  // otherwise padding, which the last range has marked
-#pragma unroll 4
-      for (int64_t r = r0; r <= r1; ++r) {
-        const float2 ml = pp.ml_ws[part_of(r)];
-        const float w = ml.x > -INFINITY ? fast_exp2(ml.x - top) : 0.f;
-        const f32x4 x = *reinterpret_cast<const f32x4*>(pp.o_ws + part_of(r) * kHeadDim + d);
-        sum = fmaf(w, ml.y, sum);
-        if (w > 0.f) o += w * x;
+  for (int off = kJoinLanes / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+  f32x4 o[kJoinParts] = {};
+  float sum = 0.f;
+  if (top < INFINITY) {  // otherwise padding, which the last range has marked
+    for (int base = 0; base < ranges; base += kJoinLanes) {
+      if (base > 0) ml = base + lane < ranges ? pp.ml_ws[part_of(base + lane)] : none;
+      const float mine = ml.x > -INFINITY ? fast_exp2(ml.x - top) : 0.f;
+      sum = fmaf(mine, ml.y, sum);
+      const int here = ranges - base < kJoinLanes ? ranges - base : kJoinLanes;
+      auto add = [&](int i, auto at_once) __attribute__((always_inline)) {
+        f32x4 x[at_once][kJoinParts];
+#pragma unroll
+        for (int u = 0; u < at_once; ++u)
+#pragma unroll
+          for (int p = 0; p < kJoinParts; ++p)
+            x[u][p] = *reinterpret_cast<const f32x4*>(pp.o_ws + part_of(base + i + u) * kHeadDim +
+                                                      (p * kJoinLanes + lane) * 4);
+#pragma unroll
+        for (int u = 0; u < at_once; ++u) {
+          const float w = __shfl(mine, i + u, kJoinLanes);
+          if (w > 0.f) {  // what a column without tokens has written may be NaN
+#pragma unroll
+            for (int p = 0; p < kJoinParts; ++p) o[p] += w * x[u][p];
+          }
+        }
+      };
+      int i = 0;
+      for (; i + 4 <= here; i += 4) add(i, std::integral_constant<int, 4>());
+      if (i + 2 <= here) {
+        add(i, std::integral_constant<int, 2>());
+        i += 2;
       }
+      if (i < here) add(i, std::integral_constant<int, 1>());
     }
-    store4<OutT>(dst, o * (sum != 0.f ? 1.0f / sum : 0.f));
+#pragma unroll
+    for (int off = kJoinLanes / 2; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
   }
+  const float inv = sum != 0.f ? 1.0f / sum : 0.f;
+  OutT* const dst = out + (row * pp.hq + kv * pp.group.d + (col - qi * pp.group.d)) * kHeadDim;
+#pragma unroll
+  for (int p = 0; p < kJoinParts; ++p) store4<OutT>(dst + (p * kJoinLanes + lane) * 4, o[p] * inv);
 }
 
 // ------------------------------------------------------------ host
@@ -795,10 +831,10 @@ void launch_shape(const TreeArgs& a) {
   constexpr int kCols = kColsOf<kColWaves, kTiles>;
   hipLaunchKernelGGL((tree_attn_kernel<OutT, kTerms, kChange, kColWaves, kTiles>), dim3((unsigned)a.plan.ranges),
                      dim3(64 * kWaves), 0, a.stream, a.q, a.k, a.v, a.plan, static_cast<OutT*>(a.out));
-  const int tiles16 = (a.plan.max_q_len * a.plan.group.d + kJoinCols - 1) / kJoinCols;
-  const int64_t grid = (int64_t)tiles16 * a.plan.num_seqs * a.plan.hkv;
+  const int join_tiles = (a.plan.max_q_len * a.plan.group.d + kJoinCols - 1) / kJoinCols;
+  const int64_t grid = (int64_t)join_tiles * a.plan.num_seqs * a.plan.hkv;
   hipLaunchKernelGGL((tree_join_kernel<OutT, kCols>), dim3((unsigned)grid), dim3(kJoinThreads), 0, a.stream, a.plan,
-                     tiles16, static_cast<OutT*>(a.out));
+                     join_tiles, static_cast<OutT*>(a.out));
 }
 
 template <typename OutT, int kTerms, int kChange>
