@@ -159,21 +159,25 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kernel(const uint16_t* 
   __shared__ int16_t lds_up[kNodes];
 
   // this workgroup's range
-  int64_t total = 0;
-  for (int base = 0; base < pp.num_seqs; base += 64) {
+  int64_t blocks = 0, sum = 0;  // of the lane's sequence, and up to it among the wave's
+  auto count = [&](int base) __attribute__((always_inline)) {
     const int b = base + lane;
-    int64_t blocks = 0;
+    blocks = 0;
     if (b < pp.num_seqs) {
       const Seen s = seen_of(pp, b);
       blocks = (int64_t)s.blocks * tiles_of<kCols>(pp, s.drafts) * pp.hkv;
     }
-    int64_t sum = blocks;
+    sum = blocks;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
       const int64_t y = __shfl_up(sum, off);
       if (lane >= off) sum += y;
     }
-    if (blockIdx.x == 0 && wave == 0 && b < pp.num_seqs) pp.before[b] = total + sum - blocks;
+  };
+  int64_t total = 0;
+  for (int base = 0; base < pp.num_seqs; base += 64) {
+    count(base);
+    if (blockIdx.x == 0 && wave == 0 && base + lane < pp.num_seqs) pp.before[base + lane] = total + sum - blocks;
     total += uniform(__shfl(sum, 63));
   }
   const int64_t quota = quota_of(total, pp.ranges);
@@ -186,18 +190,7 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kernel(const uint16_t* 
   int b = 0;
   int64_t at = 0;  // blocks before it
   for (int base = 0; base < pp.num_seqs; base += 64) {
-    const int i = base + lane;
-    int64_t blocks = 0;
-    if (i < pp.num_seqs) {
-      const Seen s = seen_of(pp, i);
-      blocks = (int64_t)s.blocks * tiles_of<kCols>(pp, s.drafts) * pp.hkv;
-    }
-    int64_t sum = blocks;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int64_t y = __shfl_up(sum, off);
-      if (lane >= off) sum += y;
-    }
+    if (pp.num_seqs > 64) count(base);
     const unsigned long long after = __ballot(at + sum > from);
     if (after != 0) {
       const int first = __builtin_ctzll(after);
@@ -626,11 +619,13 @@ __global__ __launch_bounds__(64 * kWaves) void tree_attn_kernel(const uint16_t* 
         all_low = other > all_low ? other : all_low;
       }
       all_low = __builtin_amdgcn_readfirstlane(all_low);
-      // whole rounds of four steps; the last of them may be on empty blocks
       for (int u = first_block; u < last_block; u += kStages * kStep) {
         step(u, lds_k0, lds_v0, lds_k3, lds_v3);
+        if (u + kStep >= last_block) break;
         step(u + kStep, lds_k1, lds_v1, lds_k0, lds_v0);
+        if (u + 2 * kStep >= last_block) break;
         step(u + 2 * kStep, lds_k2, lds_v2, lds_k1, lds_v1);
+        if (u + 3 * kStep >= last_block) break;
         step(u + 3 * kStep, lds_k3, lds_v3, lds_k2, lds_v2);
       }
       // no load may land in a stage after the workgroup has gone on
