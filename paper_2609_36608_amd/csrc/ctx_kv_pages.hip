@@ -8,8 +8,9 @@
 //     pages would need no pass over the counts, but its order would follow that of the
 //     atomics.)
 //   * A resize takes three launches: the pages given back (a workgroup per row), the needs
-//     and the free pages (one workgroup: 4 bytes a page, read once or twice from L2), and
-//     the tables (a workgroup per row).
+//     and the free pages (one workgroup: 4 bytes a page, read if anything grows, and again
+//     past 65,536 pages), and the tables (a workgroup per row).  Bound by the latency of
+//     loads that follow from each other: a workgroup plans 256 rows of 512 pages in 15 us.
 //   * Compaction is in place.  A token moves to a place no later than its own, so the
 //     places that the first i tokens go to hold, of what is still needed, only these
 //     tokens themselves: a workgroup takes one head of one sequence's keys or values
@@ -151,16 +152,19 @@ __device__ __forceinline__ void plan(const Resize& a, int64_t* lds_scan) {
     x.pages = pages_of(r, want) - had + (x.again ? 1 : 0);
     return x;
   };
+  const Need own = need_of(tid);  // of the first rows, often all of them
   int64_t needed = 0;
   for (int base = 0; base < r.num_seqs; base += kPlanThreads) {
     int64_t all = 0;
-    (void)scan(need_of(base + tid).pages, lds_scan, &all);
+    (void)scan((base == 0 ? own : need_of(base + tid)).pages, lds_scan, &all);
     needed += all;
   }
   // free pages before each wave's share of them, and in all
   const int per = (int)(((int64_t)r.num_pages + kPlanThreads - 1) / kPlanThreads) * 64;  // pages of a wave
   const int64_t first = (int64_t)wave * per;
   int64_t mine = 0, free_pages = 0, before = 0;
+  const bool kept = per <= 64 * 64;  // lane j keeps which of the wave's pages 64 j .. 64 j + 63 are free
+  unsigned long long bits = 0;
   auto is_free = [&](int i) {  // a load without a branch, so that several are on their way at once
     const int64_t page = first + i + lane;
     const int32_t refs = r.refs[page < r.num_pages ? page : r.num_pages - 1];
@@ -172,7 +176,11 @@ __device__ __forceinline__ void plan(const Resize& a, int64_t* lds_scan) {
 #pragma unroll
       for (int u = 0; u < kPlanLoads; ++u) there[u] = is_free(i + 64 * u);
 #pragma unroll
-      for (int u = 0; u < kPlanLoads; ++u) mine += __builtin_popcountll(__ballot(there[u]));
+      for (int u = 0; u < kPlanLoads; ++u) {
+        const unsigned long long who = __ballot(there[u]);
+        if (lane == i / 64 + u) bits = who;
+        mine += __builtin_popcountll(who);
+      }
     }
     before = scan(lane == 0 ? mine : 0, lds_scan, &free_pages);
     before = __shfl(before, 0);
@@ -180,7 +188,7 @@ __device__ __forceinline__ void plan(const Resize& a, int64_t* lds_scan) {
   int64_t upto = 0;  // needed by the rows before these
   for (int base = 0; base < r.num_seqs; base += kPlanThreads) {
     const int b = base + tid;
-    const Need x = need_of(b);
+    const Need x = base == 0 ? own : need_of(b);
     int64_t all = 0;
     const int64_t at = upto + scan(x.pages, lds_scan, &all);
     if (b < r.num_seqs) {
@@ -192,17 +200,21 @@ __device__ __forceinline__ void plan(const Resize& a, int64_t* lds_scan) {
   }
   // the lowest free pages, as many as may be handed out
   const int64_t most = needed < free_pages ? needed : free_pages;
-  for (int i = 0; i < per && before < most; i += 64 * kPlanLoads) {
-    bool there[kPlanLoads];
+  auto hand_out = [&](int i, unsigned long long who) {
+    const int64_t at =
+        before + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u));
+    if ((who >> lane & 1) && at < most) a.fresh[at] = (int32_t)(first + i + lane);
+    before += __builtin_popcountll(who);
+  };
+  if (kept) {
+    for (int i = 0; i < per && before < most; i += 64) hand_out(i, __shfl(bits, i / 64));
+  } else {
+    for (int i = 0; i < per && before < most; i += 64 * kPlanLoads) {
+      bool there[kPlanLoads];
 #pragma unroll
-    for (int u = 0; u < kPlanLoads; ++u) there[u] = is_free(i + 64 * u);
+      for (int u = 0; u < kPlanLoads; ++u) there[u] = is_free(i + 64 * u);
 #pragma unroll
-    for (int u = 0; u < kPlanLoads; ++u) {
-      const unsigned long long who = __ballot(there[u]);
-      const int64_t at =
-          before + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u));
-      if ((who >> lane & 1) && at < most) a.fresh[at] = (int32_t)(first + i + 64 * u + lane);
-      before += __builtin_popcountll(who);
+      for (int u = 0; u < kPlanLoads; ++u) hand_out(i + 64 * u, __ballot(there[u]));
     }
   }
 }
@@ -471,8 +483,8 @@ extern "C" int ctx_kv_resize_run_paged(ctx_decode_attn* h, int32_t* block_tables
   a.copied = a.offsets + num_seqs;
   a.fresh = a.copied + num_seqs;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  // One launch for few rows of few pages: 8 rows of 64 pages 8.0 us, in three 9.5 and the time between
-  // them (a cycle of fork, two resizes and copies 33.5 us, 38.6).
+  // One launch for few rows of few pages: a cycle of fork, two resizes and copies over 8 rows of 64 pages
+  // 33.5 us, with three launches 38.6 (30.6 now, the resizes 5.6 and 11 of it).
   if (num_seqs <= kSmallRows && (int64_t)num_seqs * max_pages_per_seq <= kSmallEntries && num_pages <= kSmallPages) {
     hipLaunchKernelGGL(resize_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
     return launched();
