@@ -48,7 +48,7 @@ constexpr int kBlockElems = kBlock * kHeadDim;
 constexpr int kNowhere = 0x7ffffff0;  // a byte offset past every range
 constexpr int kHeld = 64;             // half blocks whose cache rows a wave holds
 constexpr int kMostDrafts = CTX_TREE_MAX_DRAFTS;
-constexpr int kLeastBlocks = 4;       // of a range
+constexpr int kLeastBlocks = 4;       // of a range (4 contexts of up to 1,024 tokens 21.7 us; 2: 22.0, 8: 23.0)
 
 // what a kernel changes of the scores
 enum Change { kPlain, kBias, kCap, kCapBias };
