@@ -252,8 +252,17 @@ __device__ __forceinline__ float difference(float z, float m, float factor) {
   return is_large(m, factor) ? (z - m) * factor : fmaf(z, factor, -(m * factor));
 }
 
+// m's product with the factor, rounded.  Of a difference of two such products the compiler would make one
+// product and an FMA with the other unrounded: with an unchanged maximum not 0 but the product's rounding
+// error, by which the sums would drift with every tile.
+__device__ __forceinline__ float product_of(float m, float factor) {
+  float p = m * factor;
+  asm("" : "+v"(p));
+  return p;
+}
+
 __device__ __forceinline__ void raise(Sums& a, float m, float factor) {
-  const float by = is_large(m, factor) ? (m - a.m) * factor : m * factor - a.m * factor;
+  const float by = is_large(m, factor) ? (m - a.m) * factor : product_of(m, factor) - product_of(a.m, factor);
   const float d = fminf(by, -kLeast);
   const float c = exp2_of(-d);
   a.t = c * fmaf(-d, a.s, a.t);
