@@ -240,34 +240,41 @@ struct Sums {
   float m, s, t;
 };
 
-// What a difference to m is taken from: m's product with the factor, rounded, so that d is one FMA of
-// the logit.  What the rounding adds to every d of m alike cancels, since raise() takes differences of the
-// same rounded products; from 2^30 on it may be more than 2^d holds, and d is (z - m) factor
-// instead.
-constexpr float kLargeProduct = 1073741824.f;
+// What differences to m count from, log2 units: d = (z - a) factor - b.  With a = 0 and b the rounded product of
+// m with the factor, d is one FMA of the logit; what the rounding adds to every d alike cancels, since the
+// sums, what is taken from them and the gradient count from the same number.  Past 2^24 it may be more than
+// 1 / 2, and a is m, b 0.
+struct Origin {
+  float a, b;
+  __device__ __forceinline__ bool large() const { return a != 0.f; }  // true for a NaN too
+  // below kLeast for a masked logit unless large()
+  __device__ __forceinline__ float to(float z, float factor) const { return fmaf(z - a, factor, -b); }
+};
+constexpr float kLargeProduct = 16777216.f;
 
-__device__ __forceinline__ bool is_large(float m, float factor) { return !(fabsf(m * factor) < kLargeProduct); }
-
-__device__ __forceinline__ float difference(float z, float m, float factor) {
-  return is_large(m, factor) ? (z - m) * factor : fmaf(z, factor, -(m * factor));
-}
-
-// m's product with the factor, rounded.  Of a difference of two such products the compiler would make one
-// product and an FMA with the other unrounded: with an unchanged maximum not 0 but the product's rounding
-// error, by which the sums would drift with every tile.
-__device__ __forceinline__ float product_of(float m, float factor) {
+__device__ __forceinline__ Origin origin_of(float m, float factor) {
   float p = m * factor;
+  // Rounded here: of a difference of two such products the compiler would make one product and an FMA with
+  // the other unrounded, for an unchanged maximum not 0 but the product's rounding error, by which the
+  // sums would drift with every tile.
   asm("" : "+v"(p));
-  return p;
+  return fabsf(p) < kLargeProduct ? Origin{0.f, p} : Origin{m, 0.f};
 }
 
-__device__ __forceinline__ void raise(Sums& a, float m, float factor) {
-  const float by = is_large(m, factor) ? (m - a.m) * factor : product_of(m, factor) - product_of(a.m, factor);
-  const float d = fminf(by, -kLeast);
+// Counts the sums, so far from `at`, from a maximum m on.
+__device__ __forceinline__ void raise(Sums& a, Origin& at, float m, float factor) {
+  const Origin to = origin_of(m, factor);
+  const float d = fminf(fmaf(to.a - at.a, factor, to.b - at.b), -kLeast);
   const float c = exp2_of(-d);
   a.t = c * fmaf(-d, a.s, a.t);
   a.s *= c;
   a.m = m;
+  at = to;
+}
+
+__device__ __forceinline__ void raise(Sums& a, float m, float factor) {
+  Origin at = origin_of(a.m, factor);
+  raise(a, at, m, factor);
 }
 
 __device__ __forceinline__ Sums wave_join(Sums a, float factor) {
@@ -282,7 +289,7 @@ __device__ __forceinline__ bool is_broken(const Sums& a) { return !(a.m < INFINI
 __device__ __forceinline__ bool is_empty(const Sums& a) { return a.m <= kFloor; }
 
 __device__ __forceinline__ float log_prob(const RowsArgs& a, float z, const Sums& sums, float log_s) {
-  const float d = difference(z, sums.m, a.factor);
+  const float d = origin_of(sums.m, a.factor).to(z, a.factor);
   // differences past fp32's range in log2 units alone
   return d > -1e37f ? (d - log_s) * kLn2 : (z - sums.m) * a.scale;
 }
@@ -378,6 +385,7 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(RowsArgs a) {
       row_rsrc(reinterpret_cast<const T*>(a.logits) + (int64_t)row * a.stride, row_bytes<T>(a.vocab));
 
   Sums sums{kFloor, 0.f, 0.f};
+  Origin at = origin_of(kFloor, factor);
   Best best{lds_keys + (kTop ? wave * kHeldKeys : 0), 0, 0};
   bool fresh = true;
   u32x4 next[kTileLoads];
@@ -417,7 +425,7 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(RowsArgs a) {
       for (int e = 1; e < kElems; ++e) most[r] = max_of(most[r], z[e]);
     }
     const float top = max_of(max_of(most[0], most[1]), max_of(most[2], most[3]));
-    raise(sums, max_of(sums.m, top), factor);
+    raise(sums, at, max_of(sums.m, top), factor);
     if constexpr (kTop) {
       if (fresh) best.key = first_key(top, best.keys, a.top, lane);
       fresh = false;
@@ -433,17 +441,18 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(RowsArgs a) {
       }
     }
     // The sums of a tile.  A masked logit's d of -inf would make t NaN, which the lanes of such
-    // tiles have and take the sums again with d bounded; the others save a bound per logit.
+    // tiles have and take the sums again with d bounded; the others save a bound per logit.  In waves with a
+    // lane whose product is large, as of one that has met masked logits alone, each takes its own differences.
     auto add = [&](auto large, auto bounded, float& s, float& t) __attribute__((always_inline)) {
-      const float product = sums.m * factor;
 #pragma unroll
       for (int r = 0; r < kTileLoads; ++r) {
         float z[kElems];
         unpack<T>(x[r], z);
 #pragma unroll
         for (int e = 0; e < kElems; ++e) {
-          float d = large ? (z[e] - sums.m) * factor : fmaf(z[e], factor, -product);
+          float d = large ? at.to(z[e], factor) : fmaf(z[e], factor, -at.b);
           if (bounded) d = fmaxf(d, kLeast);
+          if (large) d = z[e] <= kFloor ? kLeast : d;
           const float w = exp2_of(d);
           s += w;
           if (kEntropy) t = fmaf(w, d, t);
@@ -453,7 +462,7 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(RowsArgs a) {
     float s = 0.f, t = 0.f;
     const std::true_type yes;
     const std::false_type no;
-    if (!__any(is_large(sums.m, factor))) {
+    if (!__any(at.large())) {
       add(no, no, s, t);
       if (kEntropy && __any(t != t)) {
         s = t = 0.f;
@@ -618,11 +627,12 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(GradArgs a) {
   const float h = kEntropy && live ? a.entropy[row] : 0.f;
   const float c0 = st.x == st.x ? -a.scale * (kEntropy ? fmaf(by_h, h, by) : by) : NAN;
   const float c1 = kEntropy ? -a.scale * by_h * kLn2 : 0.f;
-  const float product = st.x * a.factor;
-  const bool large = is_large(st.x, a.factor);
+  const Origin at = origin_of(st.x, a.factor);
+  const bool large = at.large();
   // log2 of a probability
   auto log2_p = [&](float z) __attribute__((always_inline)) {
-    return fmaxf((large ? (z - st.x) * a.factor : fmaf(z, a.factor, -product)) - log_s, kLeast);
+    if (large) return z <= kFloor ? kLeast : fmaxf(at.to(z, a.factor) - log_s, kLeast);
+    return fmaxf(fmaf(z, a.factor, -at.b) - log_s, kLeast);
   };
   auto weight = [&](float z) __attribute__((always_inline)) {
     const float d = log2_p(z);

@@ -111,3 +111,55 @@ def test_many_tiles(dtype, offset, temperature, copies):
     std = max(2.5, abs(offset) / (2e7 if dtype == "f32" else 200))
     z = (torch.randn(3, VOCAB, generator=g) * std + offset).to(DTYPES[dtype]).cuda()
     check(z, copies, temperature)
+
+
+@pytest.mark.parametrize("dtype,offset", [("f32", 1e7), ("f32", -1e7), ("f32", 1e5), ("bf16", 3000.0)])
+@pytest.mark.parametrize("copies", [1, 700], ids=["shares", "whole rows"])
+@pytest.mark.parametrize("vocab", [16384, VOCAB])
+def test_lanes_with_masked_logits_alone(vocab, copies, dtype, offset):
+    """Lanes whose every logit is masked, beside others of the same wave: each lane's terms, and what is
+    taken from their sums, count from the same number."""
+    g = torch.Generator().manual_seed(18)
+    std = max(2.5, abs(offset) / (2e7 if dtype == "f32" else 200))
+    z = torch.randn(3, vocab, generator=g) * std + offset
+    lane = torch.arange(vocab) // (16 // DTYPES[dtype].itemsize) % 64
+    z[0, lane % 2 == 0] = -math.inf
+    z[1, lane != 5] = torch.finfo(torch.bfloat16).min
+    z[2, lane == 63] = -1e38 * 1.01
+    z[2, :vocab // 2] = -math.inf
+    check(z.to(DTYPES[dtype]).cuda(), copies, 1.0)
+
+
+def test_products_either_side_of_the_large_ones():
+    """Lanes whose largest products lie on either side of 2^24, where differences to them are taken
+    in another way, in one wave and in one lane's tiles."""
+    g = torch.Generator().manual_seed(19)
+    at = 2.0 ** 24 * math.log(2)
+    for sign in (1, -1):
+        z = (sign * at + torch.randn(3, VOCAB, generator=g) * 8).float()
+        z[1] = sign * at + (torch.arange(VOCAB) % 64 - 32).float() * 0.5
+        z[2] = sign * at + (torch.arange(VOCAB) // 4096 - 18).float()
+        check(z.cuda(), 1, 1.0)
+        check(z.cuda(), 700, 1.0)
+
+
+def test_masked_logits_near_the_others():
+    """The least scale and logits just above the masked ones."""
+    z = torch.full((3, 4100), -1e38)
+    z[:, 7] = torch.nextafter(torch.tensor(-1e38), torch.tensor(0.0))
+    z[1, 9] = z[1, 7]
+    z[2, 4099] = -9.9e37
+    z = z.cuda()
+    r = token_logprobs(z, torch.tensor([7, 9, 3], dtype=torch.int32).cuda(), temperature=1e30, top=3)
+    assert r["top_tokens"].tolist() == [[7, -1, -1], [7, 9, -1], [4099, 7, -1]]
+    ln2 = math.log(2)
+    # [2]: column 7 is 1e36 below, 1e6 in scaled units
+    assert abs(r["token_logp"][0].item()) <= 4 * U and abs(r["token_logp"][1].item() + ln2) <= 8 * U
+    assert r["token_logp"][2] == -math.inf
+    assert abs(r["entropy"][0].item()) <= 4 * U and abs(r["entropy"][1].item() - ln2) <= 8 * U and r["entropy"][2] == 0
+    by = torch.ones(3).cuda()
+    grad = token_logprobs_grad(z, torch.tensor([7, 7, 4099], dtype=torch.int32).cuda(), r, by, temperature=1e30)
+    grad = grad.double().cpu() * 1e30
+    want = torch.zeros(3, 4100, dtype=torch.float64)
+    want[1, 7], want[1, 9] = 0.5, -0.5
+    assert ((grad - want).abs() <= 16 * U).all()
