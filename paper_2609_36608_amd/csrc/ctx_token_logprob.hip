@@ -249,6 +249,8 @@ struct Origin {
   __device__ __forceinline__ bool large() const { return a != 0.f; }  // true for a NaN too
   // below kLeast for a masked logit unless large()
   __device__ __forceinline__ float to(float z, float factor) const { return fmaf(z - a, factor, -b); }
+  // how far it is past m's product itself, exact: what a row's sum in memory no longer has
+  __device__ __forceinline__ float past(float m, float factor) const { return fmaf(a - m, factor, b); }
 };
 constexpr float kLargeProduct = 16777216.f;
 
@@ -313,7 +315,10 @@ __device__ __forceinline__ void write_row(const RowsArgs& a, int row, const Sums
   if (tid == 0) {
     if (a.entropy != nullptr)
       a.entropy[row] = broken ? NAN : empty ? 0.f : kLn2 * (log_s - sums.t / sums.s);
-    if (a.stats != nullptr) reinterpret_cast<float2*>(a.stats)[row] = broken ? make_float2(NAN, NAN) : make_float2(sums.m, empty ? 0.f : sums.s);
+    if (a.stats != nullptr) {
+      const float s = sums.s * exp2_of(origin_of(sums.m, a.factor).past(sums.m, a.factor));
+      reinterpret_cast<float2*>(a.stats)[row] = broken ? make_float2(NAN, NAN) : make_float2(sums.m, empty ? 0.f : s);
+    }
   }
 }
 
@@ -622,13 +627,13 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(GradArgs a) {
       any = lds_by[i] != 0.f ? 1.f : any;  // a NaN too
     }
   }
-  // p (c0 + c1 log2 p) with log2 p = x - m - log2 s:  -scale p (by + by_h (ln p + entropy))
-  const float log_s = __log2f(st.y);
+  // p (c0 + c1 log2 p) with log2 p = d - log2 s:  -scale p (by + by_h (ln p + entropy))
+  const Origin at = origin_of(st.x, a.factor);
+  const bool large = at.large();
+  const float log_s = __log2f(st.y) - at.past(st.x, a.factor);
   const float h = kEntropy && live ? a.entropy[row] : 0.f;
   const float c0 = st.x == st.x ? -a.scale * (kEntropy ? fmaf(by_h, h, by) : by) : NAN;
   const float c1 = kEntropy ? -a.scale * by_h * kLn2 : 0.f;
-  const Origin at = origin_of(st.x, a.factor);
-  const bool large = at.large();
   // log2 of a probability
   auto log2_p = [&](float z) __attribute__((always_inline)) {
     if (large) return z <= kFloor ? kLeast : fmaxf(at.to(z, a.factor) - log_s, kLeast);

@@ -163,3 +163,21 @@ def test_masked_logits_near_the_others():
     want = torch.zeros(3, 4100, dtype=torch.float64)
     want[1, 7], want[1, 9] = 0.5, -0.5
     assert ((grad - want).abs() <= 16 * U).all()
+
+
+@pytest.mark.parametrize("copies", [1, 700], ids=["shares", "whole rows"])
+@pytest.mark.parametrize("dtype,offset,temperature", CASES)
+def test_stats(dtype, offset, temperature, copies):
+    """The largest logit, and the sum of exp(x - scale * that) of the row."""
+    g = torch.Generator().manual_seed(20)
+    std = max(2.5, abs(offset) / (2e7 if dtype == "f32" else 200))
+    z = (torch.randn(3, VOCAB, generator=g) * std + offset).to(DTYPES[dtype]).cuda()
+    e = Exact(z, temperature)
+    stats = token_logprobs(z.repeat(copies, 1), temperature=temperature)["stats"][:3]
+    assert torch.equal(stats[:, 0], z.float().amax(1))
+    # its logarithm is off as log s is, and by an exp2 and a product more
+    within(stats[:, 1].double().log(), e.s.log(), e.log_tol + 4 * U, "log of the sum")
+    # a row's log sum exp follows from them
+    x = z.double() / temperature
+    lse = stats[:, 0].double() / temperature + stats[:, 1].double().log()
+    within(lse - x.amax(1), torch.logsumexp(x - x.amax(1, keepdim=True), 1), e.log_tol + 4 * U, "log sum exp")
