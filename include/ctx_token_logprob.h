@@ -66,6 +66,7 @@ int ctx_token_logprob_workspace(ctx_dtype dtype, int32_t vocab, int32_t num_rows
  *   tokens      int32 [num_rows, num_tokens], or NULL with num_tokens = 0
  *   num_tokens  0 .. CTX_LOGPROB_MAX_TOKENS
  *   mask        uint8 [num_rows], zero: a masked row; NULL: none is
+ *   num_rows    0 .. 2^24 - 1
  *   scale       1e-30 .. 1e30
  *   top         0 .. CTX_LOGPROB_MAX_TOP
  *   token_logp  float [num_rows, num_tokens] out (NULL with num_tokens = 0)
@@ -75,7 +76,7 @@ int ctx_token_logprob_workspace(ctx_dtype dtype, int32_t vocab, int32_t num_rows
  *   top_tokens, top_logp  int32 and float [num_rows, top] out (NULL with top = 0)
  *   workspace   at least what ctx_token_logprob_workspace says, 16-byte aligned; calls
  *               that may overlap need one each.  NULL if that is 0
- * Errors: INVALID_ARG, UNSUPPORTED (vocab, num_tokens, top), CAPACITY (workspace_bytes),
+ * Errors: INVALID_ARG, UNSUPPORTED (vocab, num_tokens, num_rows, top), CAPACITY (workspace_bytes),
  * ALIGNMENT (16 bytes: logits, workspace), HIP.
  */
 int ctx_token_logprob_run(const void* logits, ctx_dtype dtype, int64_t row_stride, int32_t vocab, const int32_t* tokens,

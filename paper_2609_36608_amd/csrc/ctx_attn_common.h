@@ -152,6 +152,9 @@ int hip_fail(hipError_t e, const char* what) {
 
 bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0; }
 
+// Whether a launch's x dimension holds `groups` workgroups: its threads are counted in 32 bits.
+[[maybe_unused]] bool fits_launch(int64_t groups, int threads) { return groups <= 0xffffffffll / threads; }
+
 inline int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 // Checks shared by every call on a handle; they clear the last error first.

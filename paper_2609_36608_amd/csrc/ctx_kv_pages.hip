@@ -423,6 +423,7 @@ int check_rows(ctx_decode_attn* h, int32_t num_seqs, int32_t max_pages, int32_t 
     return fail(CTX_ERR_INVALID_ARG, "num_pages must not be negative and max_pages_per_seq must be positive");
   if ((int64_t)num_pages * h->desc.page_tokens > kMostTokens)
     return fail(CTX_ERR_UNSUPPORTED, "caches of more than %d tokens", kMostTokens);
+  if (!fits_launch(num_seqs, kRowThreads)) return fail(CTX_ERR_INVALID_ARG, "grid of rows too large");
   return CTX_OK;
 }
 
@@ -504,10 +505,10 @@ extern "C" int ctx_kv_copy_run_paged(ctx_decode_attn* h, void* k_pages, void* v_
   if (k_pages == nullptr || v_pages == nullptr || copies == nullptr) return fail(CTX_ERR_INVALID_ARG, "NULL data pointer");
   if (!aligned16(k_pages) || !aligned16(v_pages) || (reinterpret_cast<uintptr_t>(copies) & 7u) != 0)
     return fail(CTX_ERR_ALIGNMENT, "k_pages and v_pages must be 16-byte and copies 8-byte aligned");
-  if ((rc = check_device(h)) != CTX_OK) return rc;
   const int64_t page_bytes = (int64_t)h->desc.page_tokens * h->desc.num_kv_heads * kHeadDim * 2;
   const int64_t parts = (page_bytes + kCopyChunk - 1) / kCopyChunk;
-  if (parts * num_copies > kMostTokens) return fail(CTX_ERR_INVALID_ARG, "copy grid too large");
+  if (!fits_launch(parts * num_copies, kCopyThreads)) return fail(CTX_ERR_INVALID_ARG, "copy grid too large");
+  if ((rc = check_device(h)) != CTX_OK) return rc;
   hipLaunchKernelGGL(copy_kernel, dim3((unsigned)(parts * num_copies), 2), dim3(kCopyThreads), 0,
                      reinterpret_cast<hipStream_t>(stream), static_cast<uint16_t*>(k_pages),
                      static_cast<uint16_t*>(v_pages), copies, num_pages, page_bytes, (int32_t)parts);
@@ -530,6 +531,8 @@ extern "C" int ctx_kv_compact_run_paged(ctx_decode_attn* h, void* k_pages, void*
     return fail(CTX_ERR_INVALID_ARG, "new_lens may not be an input");
   if (!aligned16(k_pages) || !aligned16(v_pages))
     return fail(CTX_ERR_ALIGNMENT, "k_pages and v_pages must be 16-byte aligned");
+  const int64_t grid = (int64_t)num_seqs * 2 * h->desc.num_kv_heads;
+  if (!fits_launch(grid, kMoveThreads)) return fail(CTX_ERR_INVALID_ARG, "compaction grid too large");
   if ((rc = check_device(h)) != CTX_OK) return rc;
   Compact a{};
   a.k = static_cast<uint16_t*>(k_pages);
@@ -546,8 +549,6 @@ extern "C" int ctx_kv_compact_run_paged(ctx_decode_attn* h, void* k_pages, void*
   a.hkv = h->desc.num_kv_heads;
   a.total_q = total_q;
   a.new_lens = new_lens;
-  const int64_t grid = (int64_t)num_seqs * 2 * a.hkv;
-  if (grid > kMostTokens) return fail(CTX_ERR_INVALID_ARG, "compaction grid too large");
   hipLaunchKernelGGL(compact_kernel, dim3((unsigned)grid), dim3(kMoveThreads), 0, reinterpret_cast<hipStream_t>(stream), a);
   return launched();
 }

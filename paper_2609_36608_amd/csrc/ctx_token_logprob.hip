@@ -51,6 +51,7 @@ constexpr int kMostTokens = CTX_LOGPROB_MAX_TOKENS;
 constexpr int kHeldKeys = 128;                     // of a wave: the best and up to 64 more
 constexpr int kMostSplits = 64;
 constexpr int32_t kMostVocab = 1 << 28;
+constexpr int32_t kMostGroups = 0xffffffffu / kThreads;  // of a launch, whose threads are counted in 32 bits
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kFloor = -1e38f;  // logits up to here are masked
@@ -716,7 +717,7 @@ int check_shape(ctx_dtype dtype, int32_t vocab, int32_t num_rows) {
   if (vocab <= 0) return fail(CTX_ERR_INVALID_ARG, "vocab %d <= 0", vocab);
   if (vocab > kMostVocab) return fail(CTX_ERR_UNSUPPORTED, "vocab %d > %d", vocab, kMostVocab);
   if (num_rows < 0) return fail(CTX_ERR_INVALID_ARG, "num_rows %d < 0", num_rows);
-  if (num_rows > 1 << 24) return fail(CTX_ERR_UNSUPPORTED, "num_rows %d > %d", num_rows, 1 << 24);
+  if (num_rows > kMostGroups) return fail(CTX_ERR_UNSUPPORTED, "num_rows %d > %d", num_rows, kMostGroups);
   return CTX_OK;
 }
 
@@ -905,7 +906,7 @@ extern "C" int ctx_token_logprob_grad_run(const void* logits, ctx_dtype dtype, i
   // tiles gain nothing: half 203).
   const int64_t chunks = (vocab + chunk_of(dtype) - 1) / chunk_of(dtype);
   const int64_t tiles = (chunks + kTileLoads * kThreads - 1) / (kTileLoads * kThreads);
-  const int64_t most = ((int64_t)1 << 30) / num_rows;
+  const int64_t most = kMostGroups / num_rows;
   a.splits = (int32_t)(tiles < most ? tiles : most);
   const dim3 grid((unsigned)num_rows * (unsigned)a.splits), block(kThreads);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);

@@ -815,7 +815,7 @@ int check_drafts(const ctx_decode_attn* h, int32_t num_seqs, int32_t max_q_len) 
   if (max_q_len < 0) return fail(CTX_ERR_INVALID_ARG, "max_q_len %d < 0", max_q_len);
   if (max_q_len > kMostDrafts) return fail(CTX_ERR_UNSUPPORTED, "max_q_len %d > %d", max_q_len, kMostDrafts);
   const int64_t tiles = ((int64_t)max_q_len * (h->desc.num_q_heads / h->desc.num_kv_heads) + kJoinCols - 1) / kJoinCols;
-  if (tiles * num_seqs * h->desc.num_kv_heads > kMostTokens) return fail(CTX_ERR_INVALID_ARG, "tree grid too large");
+  if (!fits_launch(tiles * num_seqs * h->desc.num_kv_heads, kJoinThreads)) return fail(CTX_ERR_INVALID_ARG, "tree grid too large");
   return CTX_OK;
 }
 
