@@ -21,7 +21,8 @@
  *                 caller sets it up (zeros, if all rows are empty) and leaves it to
  *                 ctx_kv_fork_run_paged and ctx_kv_resize_run_paged
  * An entry outside 0 .. num_pages - 1 is no fault: it holds no page, and no token is read or
- * written there.
+ * written there.  Arrays that a call writes may not overlap each other or those that it
+ * reads, unless said otherwise (INVALID_ARG).
  *
  * Conventions as in ctx_decode_attn.h: device pointers unless stated, owned by the
  * caller until the work queued on `stream` completes; asynchronous, no allocation, no
@@ -67,7 +68,8 @@ size_t ctx_kv_resize_workspace(int32_t num_seqs, int32_t num_pages);
  * later one that needs pages, keeps its length and pages; so does one whose new length is past
  * max_pages_per_seq * P.  Pages replaced in this call are free in the next.
  *
- *   granted  int32 [num_seqs] out: the rows' lengths from now on.  May be seq_lens or new_lens
+ *   granted  int32 [num_seqs] out: the rows' lengths from now on.  May be seq_lens or new_lens,
+ *            the same array and no part of it
  *   copies   int32 [num_seqs, 2] out: the page that was replaced and the one in its
  *            place, whose data ctx_kv_copy_run_paged has to copy; -1, -1 where none was
  *   workspace, workspace_bytes  at least ctx_kv_resize_workspace, 16-byte aligned; calls that
@@ -105,7 +107,6 @@ int ctx_kv_copy_run_paged(ctx_decode_attn* handle, void* k_pages, void* v_pages,
  *               entries that do not rise
  *   keep_lens   int32 [num_seqs], 0 .. q_lens[b]
  *   new_lens    int32 [num_seqs] out, or NULL: seq_lens[b] - q_lens[b] + keep_lens[b].
- *               May not overlap the inputs
  * Pages that tokens move within or to must not be shared with other sequences.  Tables and
  * counts stay as they are: ctx_kv_resize_run_paged to new_lens gives pages back.
  * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, ALIGNMENT (16 bytes: pages), HIP.

@@ -432,6 +432,26 @@ Rows rows_of(const ctx_decode_attn* h, int32_t* tables, int32_t max_pages, int32
   return Rows{tables, max_pages, h->desc.page_tokens, num_seqs, refs, num_pages};
 }
 
+// Whether two arrays of 32-bit values share any.
+bool overlap(const void* a, int64_t a_values, const void* b, int64_t b_values) {
+  const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+  return a_values > 0 && b_values > 0 && p < q + (uintptr_t)b_values * 4 && q < p + (uintptr_t)a_values * 4;
+}
+
+struct Array {
+  const void* data;
+  int64_t values;
+};
+
+// Whether one of the arrays that a call writes, the first `written` ones, shares values with another of them all.
+template <int kArrays>
+bool any_overlap(const Array (&x)[kArrays], int written) {
+  for (int i = 0; i < written; ++i)
+    for (int j = i + 1; j < kArrays; ++j)
+      if (overlap(x[i].data, x[i].values, x[j].data, x[j].values)) return true;
+  return false;
+}
+
 int launched() {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? CTX_OK : hip_fail(e, "kernel launch");
@@ -448,6 +468,9 @@ extern "C" int ctx_kv_fork_run_paged(ctx_decode_attn* h, int32_t* block_tables, 
   if (block_tables == nullptr || seq_lens == nullptr || parents == nullptr ||
       (page_refs == nullptr && num_pages > 0))
     return fail(CTX_ERR_INVALID_ARG, "NULL data pointer");
+  const int64_t seqs = num_seqs;
+  if (any_overlap({{block_tables, seqs * max_pages_per_seq}, {seq_lens, seqs}, {page_refs, num_pages}, {parents, seqs}}, 3))
+    return fail(CTX_ERR_INVALID_ARG, "block_tables, seq_lens, page_refs and parents may not overlap");
   if ((rc = check_device(h)) != CTX_OK) return rc;
   hipLaunchKernelGGL(fork_kernel, dim3((unsigned)num_seqs), dim3(kRowThreads), 0, reinterpret_cast<hipStream_t>(stream),
                      rows_of(h, block_tables, max_pages_per_seq, num_seqs, page_refs, num_pages), seq_lens, parents);
@@ -473,6 +496,16 @@ extern "C" int ctx_kv_resize_run_paged(ctx_decode_attn* h, int32_t* block_tables
     return fail(CTX_ERR_ALIGNMENT, "workspace must be 16-byte and copies 8-byte aligned");
   const size_t need = ctx_kv_resize_workspace(num_seqs, num_pages);
   if (workspace_bytes < need) return fail(CTX_ERR_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+  const int64_t seqs = num_seqs;
+  // granted may be one of the lengths themselves
+  const bool over_lens = granted == seq_lens, over_new = granted == new_lens;
+  if (any_overlap({{block_tables, seqs * max_pages_per_seq}, {page_refs, num_pages}, {copies, 2 * seqs},
+                   {workspace, (int64_t)(need / sizeof(int32_t))}, {granted, seqs}, {seq_lens, over_lens ? 0 : seqs},
+                   {new_lens, over_new ? 0 : seqs}}, 5) ||
+      (over_lens && !over_new && overlap(seq_lens, seqs, new_lens, seqs)))
+    return fail(CTX_ERR_INVALID_ARG,
+                "block_tables, page_refs, granted, copies and workspace may not overlap each other or an input, but for "
+                "granted seq_lens or new_lens themselves");
   if ((rc = check_device(h)) != CTX_OK) return rc;
   Resize a{};
   a.rows = rows_of(h, block_tables, max_pages_per_seq, num_seqs, page_refs, num_pages);
@@ -527,12 +560,16 @@ extern "C" int ctx_kv_compact_run_paged(ctx_decode_attn* h, void* k_pages, void*
   if (k_pages == nullptr || v_pages == nullptr || block_tables == nullptr || seq_lens == nullptr || q_starts == nullptr ||
       q_lens == nullptr || keep_lens == nullptr || (keep == nullptr && total_q > 0))
     return fail(CTX_ERR_INVALID_ARG, "NULL data pointer");
-  if (new_lens != nullptr && (new_lens == seq_lens || new_lens == q_lens || new_lens == keep_lens || new_lens == q_starts))
-    return fail(CTX_ERR_INVALID_ARG, "new_lens may not be an input");
   if (!aligned16(k_pages) || !aligned16(v_pages))
     return fail(CTX_ERR_ALIGNMENT, "k_pages and v_pages must be 16-byte aligned");
   const int64_t grid = (int64_t)num_seqs * 2 * h->desc.num_kv_heads;
   if (!fits_launch(grid, kMoveThreads)) return fail(CTX_ERR_INVALID_ARG, "compaction grid too large");
+  const int64_t seqs = num_seqs;
+  if (new_lens != nullptr && any_overlap({{new_lens, seqs}, {seq_lens, seqs}, {q_starts, seqs}, {q_lens, seqs},
+                                          {keep_lens, seqs}, {keep, total_q}, {block_tables, seqs * max_pages_per_seq}}, 1))
+    return fail(CTX_ERR_INVALID_ARG, "new_lens may not overlap an input");
+  const int64_t cache = (int64_t)num_pages * h->desc.page_tokens * h->desc.num_kv_heads * kHeadDim / 2;
+  if (overlap(k_pages, cache, v_pages, cache)) return fail(CTX_ERR_INVALID_ARG, "k_pages and v_pages may not overlap");
   if ((rc = check_device(h)) != CTX_OK) return rc;
   Compact a{};
   a.k = static_cast<uint16_t*>(k_pages);
