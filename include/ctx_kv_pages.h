@@ -15,8 +15,9 @@
  * Common arguments (with those of ctx_paged_attn.h):
  *   block_tables  int32 [num_seqs, max_pages_per_seq].  Row b holds the pages of its
  *                 first ceil(seq_lens[b] / P) entries, P the handle's page_tokens
- *   seq_lens      int32 [num_seqs]: a value below 0 counts as 0, and one past the row's
- *                 max_pages_per_seq * P tokens as that
+ *   seq_lens      int32 [num_seqs]: a value below 0 counts as 0.  Forks and resizes count one past
+ *                 the row's max_pages_per_seq * P tokens as that; for a compaction the
+ *                 tokens past them are on no page
  *   page_refs     int32 [num_pages]: how many rows hold each page; 0 is a free one.  The
  *                 caller sets it up (zeros, if all rows are empty) and leaves it to
  *                 ctx_kv_fork_run_paged and ctx_kv_resize_run_paged
