@@ -7,10 +7,10 @@
 //     pages, so that what a call does depends on its inputs alone.  (A stack of free
 //     pages would need no pass over the counts, but its order would follow that of the
 //     atomics.)
-//   * A resize takes three launches: the pages given back (a workgroup per row), the needs
-//     and the free pages (one workgroup: 4 bytes a page, read if anything grows, and again
-//     past 65,536 pages), and the tables (a workgroup per row).  Bound by the latency of
-//     loads that follow from each other: a workgroup plans 256 rows of 512 pages in 15 us.
+//   * A resize of more than a few short rows takes three launches: the pages given back (a
+//     workgroup per row), the needs and the free pages (one workgroup: 4 bytes a page, read if
+//     anything grows, and again past 65,536 pages), and the tables (a workgroup per row).  Bound
+//     by the latency of loads that follow from each other: a workgroup plans 256 rows of 512 pages in 15 us.
 //   * Compaction is in place.  A token moves to a place no later than its own, so the
 //     places that the first i tokens go to hold, of what is still needed, only these
 //     tokens themselves: a workgroup takes one head of one sequence's keys or values
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(kRowThreads) void give_back_kernel(Resize a) {
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / 64;
 constexpr int kPlanLoads = 8;  // of counts, per thread at once
-constexpr int32_t kSmallRows = 64, kSmallEntries = 8192, kSmallPages = 32768;
+constexpr int32_t kSmallRows = kPlanWaves, kSmallWidth = 256;  // rows and entries of a row that one launch resizes
 
 // Sum of x over the threads before this one; *total over all.
 __device__ __forceinline__ int64_t scan(int64_t x, int64_t* lds, int64_t* total) {
@@ -258,12 +258,12 @@ __global__ __launch_bounds__(kRowThreads) void grow_kernel(Resize a) {
   grow(a, blockIdx.x, threadIdx.x, kRowThreads, [] { __syncthreads(); });
 }
 
-// All three for few rows and pages, a wave per row.
+// All three for few short rows, a wave per row.
 __global__ __launch_bounds__(kPlanThreads) void resize_kernel(Resize a) {
   __shared__ int64_t lds_scan[kPlanWaves];
   const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-  for (int b = wave; b < a.rows.num_seqs; b += kPlanWaves) give_back(a, b, lane, 64);
+  const int b = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  if (b < a.rows.num_seqs) give_back(a, b, lane, 64);
   // The counts change in L2, past this CU's cache, which may hold lines with some of them, read for
   // lengths or tables beside them: once a wave's atomics are done it drops these lines.
   __builtin_amdgcn_s_waitcnt(0);
@@ -272,7 +272,7 @@ __global__ __launch_bounds__(kPlanThreads) void resize_kernel(Resize a) {
   plan(a, lds_scan);
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
-  for (int b = wave; b < a.rows.num_seqs; b += kPlanWaves) grow(a, b, lane, 64, [] { __builtin_amdgcn_wave_barrier(); });
+  if (b < a.rows.num_seqs) grow(a, b, lane, 64, [] { __builtin_amdgcn_wave_barrier(); });
 }
 
 // ------------------------------------------------------------ copy
@@ -517,9 +517,11 @@ extern "C" int ctx_kv_resize_run_paged(ctx_decode_attn* h, int32_t* block_tables
   a.copied = a.offsets + num_seqs;
   a.fresh = a.copied + num_seqs;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  // One launch for few rows of few pages: a cycle of fork, two resizes and copies over 8 rows of 64 pages
-  // 33.5 us, with three launches 38.6 (30.6 now, the resizes 5.6 and 11 of it).
-  if (num_seqs <= kSmallRows && (int64_t)num_seqs * max_pages_per_seq <= kSmallEntries && num_pages <= kSmallPages) {
+  // One launch for few short rows, a wave each.  Growth by 40 tokens and the trim of it, with one and with three
+  // launches (us, in a graph): 8 rows of 64 entries 16.1 / 17.8, 16 17.2 / 18.3, 24 24.6 / 23.9, 64 28.7 / 19.0; of
+  // 131,072 pages 31.5 / 33.6.  Whole rows emptied and filled: 16 of 128 entries 18.0 / 18.2, of 256 20.3 / 19.1, of
+  // 512 24.8 / 21.6, one of 8,192 89 / 38.
+  if (num_seqs <= kSmallRows && max_pages_per_seq <= kSmallWidth) {
     hipLaunchKernelGGL(resize_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
     return launched();
   }

@@ -1,7 +1,9 @@
-"""Compaction of sequences longer than their rows of the block table."""
+"""Compaction of sequences longer than their rows of the block table, and resizes either side of the rule
+that chooses how many launches they take."""
 import pytest
 import torch
 
+import test_gpu_kv_pages as pages_tests
 from paper_2609_36608_amd import DecodeAttention
 from test_gpu_kv_pages import Kept, i32
 
@@ -28,3 +30,9 @@ def test_tokens_past_the_table():
                                  i32([len(t) for t in kept]))
     assert got.tolist() == [n - m + len(t) for n, m, t in zip(lens, new, kept)]
     assert torch.equal(c.k.view(torch.int16), want[0]) and torch.equal(c.v.view(torch.int16), want[1])
+
+
+@pytest.mark.parametrize("seqs,width,pages", [(16, 256, 3000), (16, 257, 3000), (17, 256, 3000), (15, 200, 70001),
+                                              (18, 200, 140003), (2, 3, 65537)])
+def test_either_side_of_one_launch(seqs, width, pages):
+    pages_tests.test_random_lives(seqs, width, 16, pages)
