@@ -26,8 +26,9 @@
  * Where a row has no more alternatives the column is -1, the log probability -inf (NaN
  * in a row of NaN, 0 in a masked one).
  *
- * Arithmetic: fp32 (differences to the largest logit in one FMA each, sums over lanes and
- * then in a fixed order); gradients are rounded to the logits' type once, nearest even.
+ * Arithmetic: fp32 (differences to the largest logit in one FMA each, or two roundings where its
+ * product is 2^24 or more, so that no result grows worse with an offset of all logits; sums over lanes
+ * and then in a fixed order); gradients are rounded to the logits' type once, nearest even.
  * Deterministic.
  *
  * Conventions as in ctx_decode_attn.h: device pointers unless stated, owned by the

@@ -53,7 +53,9 @@ int ctx_tree_attn_workspace(ctx_decode_attn* handle, int32_t num_seqs, int32_t m
  *            drafts below one: nothing of their q, keys and values is used, and they get zeros
  *   max_q_len  host bound on q_lens, up to CTX_TREE_MAX_DRAFTS; drafts past it are not touched
  *   scores   NULL: s = scale * q . k, every token.  Without doc_starts; a prefix counts up to
- *            H_b tokens.  CTX_SCORES_SPLIT_P as for the prefill
+ *            H_b tokens.  CTX_SCORES_SPLIT_P asks for two-term softmax weights with bf16
+ *            outputs; without it they are of one term, whatever the cap (the prefill takes
+ *            two for caps above 512)
  *   out      [total_q, Hq, D] of desc.out_dtype, contiguous
  *   workspace, workspace_bytes  at least what ctx_tree_attn_workspace says, 16-byte aligned;
  *            calls that may overlap need one each

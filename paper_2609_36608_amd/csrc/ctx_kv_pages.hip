@@ -10,7 +10,7 @@
 //   * A resize of more than a few short rows takes three launches: the pages given back (a
 //     workgroup per row), the needs and the free pages (one workgroup: 4 bytes a page, read if
 //     anything grows, and again past 65,536 pages), and the tables (a workgroup per row).  Bound
-//     by the latency of loads that follow from each other: a workgroup plans 256 rows of 512 pages in 15 us.
+//     by the latency of loads that follow from each other: a workgroup plans 256 rows of 512 pages in 14 us.
 //   * Compaction is in place.  A token moves to a place no later than its own, so the
 //     places that the first i tokens go to hold, of what is still needed, only these
 //     tokens themselves: a workgroup takes one head of one sequence's keys or values
@@ -322,7 +322,8 @@ struct Compact {
 
 // One workgroup per (sequence, cache, head).  What it takes is what the longest sequence's workgroups
 // take, at 30 GB/s each: 12 contexts of 8,192..16,384 tokens 208 us, 3.8 TB/s, the copy rate as
-// long as all are at work.  (Half a head per workgroup, in parts of 128 bytes: 227; a quarter: 268;
+// long as all are at work.  (Several could share a sequence's head, if each wrote its block once the
+// blocks before it had been read; that needs counters, which the call has no workspace for.)  (Half a head per workgroup, in parts of 128 bytes: 227; a quarter: 268;
 // twice the loads in flight: 209, but 0.8 us more for the accepted paths of 64 requests.)
 __global__ __launch_bounds__(kMoveThreads) void compact_kernel(Compact a) {
   __shared__ int32_t lds_from[3][kMoveTokens], lds_to[3][kMoveTokens];  // cache rows, -1: nothing to move

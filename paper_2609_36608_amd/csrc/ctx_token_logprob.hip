@@ -3,14 +3,16 @@
 // include/ctx_token_logprob.h.
 //
 // A row of V logits is read once: bound by HBM for many rows, by latency for a few.  Over
-// 151,936 bf16 logits: 4,301 rows of which 0.8 count 179 us, 5.9 TB/s; 8 rows with 20
-// alternatives 12.4 us and 6.6 for the merge; 2,057 rows and their gradient 287 us, 6.1 TB/s.
+// 151,936 bf16 logits: 4,301 rows of which 0.8 count 177 us, 6.0 TB/s (up to 253 in the first
+// milliseconds of load, while the clock falls: bound by exps as much); 8 rows with 20 alternatives 12.3 us and 6.6
+// for the merge; 2,057 rows and their gradient 286 us, 6.1 TB/s.
 //
 //   * logprob_kernel: a workgroup of 4 waves per row, or per share of a row where there
 //     are few.  Every lane keeps a running maximum m and, with d = (z - m) scale log2 e,
 //     s = sum 2^d and t = sum 2^d d, rescaled once per tile of 4 loads: raising m so
 //     that every d falls by r makes them 2^-r s and 2^-r (t - r s).  Then
 //     log sum exp x = scale m + ln2 log2 s, and the entropy is ln2 (log2 s - t / s).
+//     d counts from the rounded product of m, up to 2^24, as do all that use s and t.
 //   * Alternatives: a wave holds the best `top` it has met as 64-bit keys, the value's
 //     order above the complement of the column, so that keys differ and the larger key
 //     is the better alternative.  A chunk enters the search only if one of its values
@@ -447,8 +449,9 @@ __global__ __launch_bounds__(kThreads) void logprob_kernel(RowsArgs a) {
       }
     }
     // The sums of a tile.  A masked logit's d of -inf would make t NaN, which the lanes of such
-    // tiles have and take the sums again with d bounded; the others save a bound per logit.  In waves with a
-    // lane whose product is large, as of one that has met masked logits alone, each takes its own differences.
+    // tiles have and take the sums again with d bounded; the others save a bound per logit (4,301 whole rows
+    // 211 us, 262 with one in 64 masked, 207 either way without the entropy).  In waves with a lane whose
+    // product is large, as of one that has met masked logits alone, each takes its own differences.
     auto add = [&](auto large, auto bounded, float& s, float& t) __attribute__((always_inline)) {
 #pragma unroll
       for (int r = 0; r < kTileLoads; ++r) {

@@ -16,7 +16,8 @@
 //     through LDS at the item's end; with more, all eight hold columns.  The blocks
 //     pass through four stages of LDS tiles, loaded three steps ahead by all waves; waves
 //     without columns only load.  32 query heads on 8, bf16: 64 contexts of 2,048..8,191 with
-//     12..31 drafts 289 us, 4.8 TB/s; 32 of 512..32,767 with 64 drafts 430 us, 645 TFLOP/s.
+//     12..31 drafts 286 us, 4.9 TB/s; 32 of 512..32,767 with 64 drafts 427 us, 650 TFLOP/s (two-term
+//     weights 320 and 495).  In the first milliseconds of load, while the clock falls, up to 371 and 539.
 //     With 4 waves and two workgroups per CU 308 and 511 us; with the next block's keys read
 //     ahead, which spills registers for fp32 outputs, 308 and 380 (290 and 425 at that time).
 //   * Trees: the ancestors of every draft, as a mask of bits, by doubling: with the ancestors up
